@@ -28,6 +28,13 @@
  *   spade_candidate_sics     SICS of every candidate blocking in one pass
  *   spade_aggregation_score  per-head Aggregation Score of one candidate scheme
  *   spade_choose_scheme      per-head argmax over the candidates
+ * and attention over a paged key/value cache, for tokens that arrive in a stream
+ * (video generated chunk of frames after chunk, single tokens):
+ *   spade_cache_append       new keys and values into pages (bf16 or 4 bits), with the
+ *                            position rotation of keys and queries on the way
+ *   spade_cache_select       Top-K pages for every query, by the pages' mean keys
+ *   spade_cache_attn         attention of every query over its pages, or over all
+ *   spade_cache_read         cached tokens back as raster tensors
  *
  * Conventions shared by every call
  *   - All tensor pointers are DEVICE pointers, owned by the caller, contiguous,
@@ -514,6 +521,172 @@ spade_status spade_sparse_attn_raster_multi(const spade_geom* geoms, int32_t n_g
                                             const void* k, const void* v, double scale, void* o,
                                             float* lse, void* workspace, size_t workspace_bytes,
                                             hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Paged key/value cache.
+ *
+ * Keys and values of a sequence live in pages of `page` tokens, taken from one pool
+ * that all sequences share: token n of sequence b is token n % page of physical page
+ * table[b][n / page]. A page holds every K/V head. Use, per layer call:
+ * spade_cache_append (the new tokens enter, the queries are rotated), then
+ * spade_cache_select and spade_cache_attn with its lists, or spade_cache_attn without
+ * lists. Query heads share K/V heads in groups: query head hq reads K/V head
+ * hq / (Hq / H).
+ *
+ * Conventions of these calls, beside those above:
+ *   - New tokens of all sequences are packed in one row dimension, token-major:
+ *     q [n_tokens, Hq, d], k and v [n_tokens, H, d]. Sequence b's are rows
+ *     cu[b]..cu[b+1]-1, the last cu[b+1] - cu[b] tokens of its lens[b] cached ones.
+ *     Rows before cu[0] or from cu[B] on belong to no sequence: outputs there are left
+ *     as they were.
+ *   - table, lens and cu are device memory and not known to the host; values that break
+ *     the rules below cannot fault. lens beyond max_pages * page count as that; pages
+ *     outside [0, n_pages) hold no token (appends to them are dropped); offsets that
+ *     do not ascend, or leave [0, n_tokens], give unspecified rows.
+ *   - A page that receives tokens belongs to one sequence; full pages may be shared.
+ *   - Limits: d in {64, 128}; page a multiple of 32 in [32, 256]; H <= 4096;
+ *     Hq / H <= 128; n_pages * page < 2^31; B <= 2^20; n_tokens <= 2^28; max_pages <=
+ *     2^23, and <= 16384 for selections and attention with lists. B or n_tokens equal
+ *     to 0 is an empty problem.
+ */
+enum { SPADE_CACHE_BF16 = 0, SPADE_CACHE_FP4 = 1 };  /* formats of a cache */
+
+/*
+ * The cache's buffers (device memory, 16-byte aligned, owned by the caller). With P =
+ * page, contents in the order the matrix instructions read them (row-major shapes;
+ * [n_pages, H] in front of each):
+ *   BF16: k [P/16][d/32][4][16][8]: token 16 i0 + i3, channel 32 i1 + 8 i2 + i4
+ *         v [P/32][d/16][4][16][2][4]: token 32 i0 + 16 i4 + 4 i2 + i5, channel 16 i1 + i3
+ *   FP4:  each group of 32 channels of a token holds e2m1 values (0, .5, 1, 1.5, 2, 3,
+ *         4, 6, bit 3 the sign) times 2^(scale - 127), scale the group's byte. e is the
+ *         least exponent >= -126 with max |x| <= 7 2^e, rounding is to nearest, ties to
+ *         even (6 2^e is the last value; at e = 126 it is 3 2^e). A group that holds a
+ *         NaN or an infinity has scale 255 and reads as NaN.
+ *         k bytes [P/16][4][16][d/8]: token 16 i0 + i2, channels (d/4) i1 + 2 i3 (low
+ *           nibble) and + 1
+ *         v bytes [P/32][d/64][4][16][4][4]: channel 64 i1 + 16 i4 + i3; low nibble, then
+ *           high: tokens 32 i0 + 4 i2 + t with t = 0..3 (bytes 0, 1), 16..19 (bytes 2, 3)
+ *         k_scale bytes [P/16][d/32][16], v_scale bytes [P/32][4][d/32][2][4]: tokens as
+ *           above
+ *   k_mean: bf16 [d]: mean of the page's stored keys (summed in fp64, rounded to fp32,
+ *         then to bf16), kept by spade_cache_append.
+ */
+typedef struct {
+  int32_t format;      /* SPADE_CACHE_BF16 | SPADE_CACHE_FP4 */
+  int32_t H, d;        /* K/V heads, head dimension */
+  int32_t page;        /* tokens per page */
+  int32_t n_pages;     /* pages in the pool */
+  void* k;
+  void* v;
+  void* k_mean;        /* spade_cache_append and _select; may be null for the others */
+  void* k_scale;       /* FP4 only */
+  void* v_scale;
+} spade_cache;
+
+/* The sequences of one call. */
+typedef struct {
+  int32_t B;             /* sequences */
+  int32_t max_pages;     /* row length of table (>= 1) */
+  int32_t n_tokens;      /* rows of the call's packed tensors */
+  const int32_t* table;  /* device int32 [B, max_pages]: physical pages */
+  const int32_t* lens;   /* device int32 [B]: tokens in the cache, new ones among them */
+  const int32_t* cu;     /* device int32 [B + 1]: rows of the new tokens, ascending */
+} spade_batch;
+
+/* Position rotation: channels a and b of a pair become a cos - b sin and a sin + b cos,
+ * with row p and column i of the tables for a token at position p: fp32, each operation
+ * rounded, then bf16. */
+typedef struct {
+  int32_t n_pos;         /* rows of the tables */
+  int32_t rot;           /* rotated channels: the first rot (a multiple of 16, <= d) */
+  int32_t interleaved;   /* 1: pair i is (2i, 2i + 1); 0: (i, i + rot / 2) */
+  const float* cos;      /* device fp32 [n_pos, rot / 2] */
+  const float* sin;
+  const int32_t* pos;    /* device int32 [n_tokens], nullable: the token's place in its
+                            sequence. Tokens outside the tables are not rotated. */
+} spade_rope;
+
+/*
+ * Appends new keys and values to their sequences' pages, and rotates keys and queries.
+ *
+ *   k, v:     bf16 [n_tokens, H, d], token rows k_stride (v_stride) elements apart (a
+ *             multiple of 8, >= H d): slices of a fused projection are taken as they are.
+ *   q, q_out: nullable (both or neither, Hq = 0 then). q bf16 [n_tokens, Hq, d], rows
+ *             q_stride elements apart; q_out contiguous, rotated (copied where nothing
+ *             rotates). q_out may be q where q is contiguous.
+ *   rope:     nullable (host struct): no rotation.
+ *   Rotated keys are rounded to bf16, then stored in the cache's format; values are
+ *   stored as they come. The means of the touched pages are taken anew from all keys
+ *   the page then holds, so tokens may also be written again (lens set back).
+ *   Needs the older tokens of touched pages in place.
+ */
+spade_status spade_cache_append(const spade_cache* c, const spade_batch* b, const void* k,
+                                int64_t k_stride, const void* v, int64_t v_stride, const void* q,
+                                int64_t q_stride, int32_t Hq, void* q_out, const spade_rope* rope,
+                                hipStream_t stream);
+
+/*
+ * Cached tokens as raster tensors, what the raster attention calls take.
+ *
+ *   k, v:  out, bf16 [B, H, N, d]: token n < min(lens[b], N, max_pages * page) of every
+ *          sequence (4-bit values are exact in bf16). Rows from there on, and tokens
+ *          on pages outside the pool, are left as they were.
+ *   b:     cu and n_tokens are not used.
+ */
+spade_status spade_cache_read(const spade_cache* c, const spade_batch* b, int64_t N, void* k, void* v,
+                              hipStream_t stream);
+
+/* Scratch bytes of spade_cache_select and spade_cache_attn (sizes only; topk as in the
+ * call, 0 for attention without lists); 0 for an empty problem or invalid arguments. */
+size_t spade_cache_select_workspace_bytes(const spade_cache* c, const spade_batch* b, int32_t Hq,
+                                          int32_t topk);
+size_t spade_cache_attn_workspace_bytes(const spade_cache* c, const spade_batch* b, int32_t Hq,
+                                        int32_t topk);
+
+/*
+ * Top-K pages of every query and K/V head, by a cheap score: the mean estimate of the
+ * block selection, with the query side summed over the heads that share a K/V head.
+ *
+ *   score(t, h, j) = sum_c (sum_g q[t, h Hq/H + g, c]) k_mean[page j, h, c], in fp64.
+ *   causal: 1: query i of sequence b's n sees the first lens[b] - n + i + 1 tokens; 0: all
+ *           lens[b]. A page is visible when one of its tokens is.
+ *   Kept: min(topk, visible) pages: the first `sink` and the last `local` visible ones,
+ *           then by (score descending, index ascending), a NaN score after all others.
+ *           sink + local <= topk; causal needs local >= 1 (the own page's mean may
+ *           hold tokens that the query must not see).
+ *   q:       bf16 [n_tokens, Hq, d] (q_out of the append).
+ *   counts:  out, int32 [n_tokens, H].
+ *   indices: out, int32 [n_tokens, H, topk]: page numbers inside the sequence, ascending,
+ *            in entries 0..counts-1; later entries are not written.
+ *   workspace: spade_cache_select_workspace_bytes bytes, 16-byte aligned; serves one
+ *            call at a time.
+ */
+spade_status spade_cache_select(const spade_cache* c, const spade_batch* b, const void* q, int32_t Hq,
+                                int32_t topk, int32_t sink, int32_t local, int32_t causal,
+                                int32_t* counts, int32_t* indices, void* workspace,
+                                size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Attention of every query over cached tokens:
+ *   o = softmax(scale q k^T) v over the visible tokens (causal as in spade_cache_select)
+ *   on the listed pages, or on all pages without lists (counts, indices null, topk 0).
+ *
+ *   counts, indices: int32 [n_tokens, H] and [n_tokens, H, topk]. A list is a set of pages:
+ *            any order; entries that are not visible pages are skipped, an entry listed
+ *            twice counts once, counts are clamped to [0, topk].
+ *   q, o:    bf16 [n_tokens, Hq, d]; a query that sees no token gets o = 0, lse = -inf.
+ *   lse:     out, nullable, fp32 [n_tokens, Hq]: natural log of the softmax denominator.
+ *   scale:   in [1e-30, 1e30].
+ *   workspace: spade_cache_attn_workspace_bytes bytes, 16-byte aligned; serves one call
+ *            at a time (it holds partial results where few rows are split over the chip).
+ *   bf16 MFMA with fp32 accumulation; softmax in fp32; P rounded to bf16 for the P*V
+ *   product. Tokens that a query does not see never reach its result, whatever they
+ *   hold. Deterministic.
+ */
+spade_status spade_cache_attn(const spade_cache* c, const spade_batch* b, const void* q, int32_t Hq,
+                              const int32_t* counts, const int32_t* indices, int32_t topk,
+                              int32_t causal, double scale, void* o, float* lse, void* workspace,
+                              size_t workspace_bytes, hipStream_t stream);
 
 /* Static, human-readable name of a status code. */
 const char* spade_status_string(spade_status s);

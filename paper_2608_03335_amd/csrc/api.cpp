@@ -9,6 +9,7 @@
 #include <utility>
 
 #include "spade.h"
+#include "cache.h"
 #include "spade_internal.h"
 
 namespace spade {
@@ -138,6 +139,68 @@ spade_status sparse_attn(const spade_geom* g, const void* q, const void* k, cons
                                                     lse, workspace, raster, stream),
                     "sparse attention launch");
 }
+// Checks a paged cache's sizes and fills `dc`.
+spade_status check_cache(const spade_cache* c, spade::DevCache* dc) {
+  if (!c) return fail(SPADE_ERR_INVALID_ARG, "cache pointer is null");
+  if (c->format != SPADE_CACHE_BF16 && c->format != SPADE_CACHE_FP4)
+    return fail(SPADE_ERR_INVALID_ARG, "cache format must be SPADE_CACHE_BF16 or SPADE_CACHE_FP4 (got %d)",
+                c->format);
+  if (c->H < 1 || c->n_pages < 1)
+    return fail(SPADE_ERR_INVALID_ARG, "a cache needs heads and pages (H=%d n_pages=%d)", c->H, c->n_pages);
+  if (c->d != 64 && c->d != 128)
+    return fail(SPADE_ERR_UNSUPPORTED, "head dim d=%d not supported (64 or 128)", c->d);
+  if (c->page < 32 || c->page > 256 || c->page % 32 != 0)
+    return fail(SPADE_ERR_UNSUPPORTED, "page=%d must be a multiple of 32 in [32, 256]", c->page);
+  if (c->H > 4096 || int64_t(c->n_pages) * c->page > (int64_t(1) << 31) - 1)
+    return fail(SPADE_ERR_UNSUPPORTED, "cache too large (H=%d n_pages=%d page=%d)", c->H, c->n_pages,
+                c->page);
+  dc->H = c->H;
+  dc->page = c->page;
+  dc->n_pages = c->n_pages;
+  dc->fp4 = c->format == SPADE_CACHE_FP4;
+  dc->k = c->k;
+  dc->v = c->v;
+  dc->ks = (uint8_t*)c->k_scale;
+  dc->vs = (uint8_t*)c->v_scale;
+  dc->mean = c->k_mean;
+  return SPADE_OK;
+}
+
+spade_status check_cache_pointers(const spade::DevCache& c, bool pages, bool mean) {
+  if (pages && (!c.k || !c.v || (c.fp4 && (!c.ks || !c.vs))))
+    return fail(SPADE_ERR_INVALID_ARG, "the cache's k and v (4 bits: k_scale and v_scale too) must be non-null");
+  if (mean && !c.mean) return fail(SPADE_ERR_INVALID_ARG, "the cache's k_mean must be non-null");
+  if (!aligned16(c.k) || !aligned16(c.v) || !aligned16(c.mean) || (c.fp4 && (!aligned16(c.ks) || !aligned16(c.vs))))
+    return fail(SPADE_ERR_INVALID_ARG, "the cache's buffers must be 16-byte aligned");
+  return SPADE_OK;
+}
+
+// Checks a batch's sizes and fills `db`.
+spade_status check_batch(const spade_batch* b, spade::DevBatch* db) {
+  if (!b) return fail(SPADE_ERR_INVALID_ARG, "batch pointer is null");
+  if (b->B < 0 || b->n_tokens < 0 || b->max_pages < 1)
+    return fail(SPADE_ERR_INVALID_ARG, "bad batch (B=%d n_tokens=%d max_pages=%d)", b->B, b->n_tokens,
+                b->max_pages);
+  if (b->B > (1 << 20) || b->n_tokens > (1 << 28) || b->max_pages > (1 << 23))
+    return fail(SPADE_ERR_UNSUPPORTED, "batch too large (B=%d n_tokens=%d max_pages=%d)", b->B,
+                b->n_tokens, b->max_pages);
+  db->B = b->B;
+  db->max_pages = b->max_pages;
+  db->n_tokens = b->n_tokens;
+  db->table = b->table;
+  db->lens = b->lens;
+  db->cu = b->cu;
+  return SPADE_OK;
+}
+
+spade_status check_group(int32_t Hq, int32_t H) {
+  if (Hq < 1 || Hq % H != 0)
+    return fail(SPADE_ERR_INVALID_ARG, "Hq=%d must be a positive multiple of the cache's H=%d", Hq, H);
+  if (Hq / H > spade::kCacheMaxGroup)
+    return fail(SPADE_ERR_UNSUPPORTED, "Hq / H = %d exceeds %d", Hq / H, spade::kCacheMaxGroup);
+  return SPADE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -678,6 +741,178 @@ spade_status spade_validate_lists(const spade_geom* g, const int32_t* counts,
   return hip_status(spade::launch_validate_lists(empty ? 0 : dg.NB, int(rows), counts, indices,
                                                  report, stream),
                     "validate_lists launch");
+}
+
+spade_status spade_cache_append(const spade_cache* c, const spade_batch* b, const void* k,
+                                int64_t k_stride, const void* v, int64_t v_stride, const void* q,
+                                int64_t q_stride, int32_t Hq, void* q_out, const spade_rope* rope,
+                                hipStream_t stream) {
+  spade::DevCache dc;
+  spade::DevBatch db;
+  spade_status st = check_cache(c, &dc);
+  if (st == SPADE_OK) st = check_batch(b, &db);
+  if (st != SPADE_OK) return st;
+  const bool empty = b->B == 0 || b->n_tokens == 0;  // pointers are then not read
+  if (!empty && (q == nullptr) != (q_out == nullptr))
+    return fail(SPADE_ERR_INVALID_ARG, "q and q_out come together");
+  if (!empty && q == nullptr && Hq != 0)
+    return fail(SPADE_ERR_INVALID_ARG, "Hq must be 0 without q (got %d)", Hq);
+  if (q && (st = check_group(Hq, c->H)) != SPADE_OK) return st;
+  const int64_t kv = int64_t(c->H) * c->d;
+  if (k_stride < kv || v_stride < kv || (q && q_stride < int64_t(Hq) * c->d))
+    return fail(SPADE_ERR_INVALID_ARG, "a token stride is shorter than a token");
+  if (k_stride % 8 || v_stride % 8 || (q && q_stride % 8))
+    return fail(SPADE_ERR_INVALID_ARG, "token strides must be multiples of 8 elements");
+  if (k_stride > (int64_t(1) << 31) || v_stride > (int64_t(1) << 31) ||
+      (q && q_stride > (int64_t(1) << 31)))
+    return fail(SPADE_ERR_UNSUPPORTED, "token stride too large");
+  spade::DevRope r = {nullptr, nullptr, nullptr, 0, 0, 0};
+  if (rope) {
+    if (rope->rot < 0 || rope->rot > c->d || rope->rot % 16 != 0 || rope->n_pos < 0 ||
+        (rope->interleaved != 0 && rope->interleaved != 1))
+      return fail(SPADE_ERR_INVALID_ARG,
+                  "rope: rot=%d must be a multiple of 16 in [0, d=%d], n_pos=%d >= 0, interleaved 0 or 1",
+                  rope->rot, c->d, rope->n_pos);
+    r = {rope->cos, rope->sin, rope->pos, rope->n_pos, rope->rot, rope->interleaved};
+  }
+  if (empty) return SPADE_OK;
+  st = check_cache_pointers(dc, true, true);
+  if (st != SPADE_OK) return st;
+  if (!k || !v || !b->table || !b->lens || !b->cu)
+    return fail(SPADE_ERR_INVALID_ARG, "k, v, table, lens and cu must be non-null");
+  if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out))
+    return fail(SPADE_ERR_INVALID_ARG, "k, v, q and q_out must be 16-byte aligned");
+  if (q && q == q_out && q_stride != int64_t(Hq) * c->d)
+    return fail(SPADE_ERR_INVALID_ARG, "q_out may be q only where q is contiguous");
+  if (r.rot && (!r.cos || !r.sin || !aligned16(r.cos) || !aligned16(r.sin)))
+    return fail(SPADE_ERR_INVALID_ARG, "rope: cos and sin must be non-null and 16-byte aligned");
+  const int64_t wgs = spade::item_base(b->n_tokens, b->B, c->page, 2) * c->H * 2 +
+                      (int64_t(b->n_tokens) * Hq * (c->d / 16) + 255) / 256;
+  if (wgs > 0x7fffffff) return fail(SPADE_ERR_UNSUPPORTED, "batch too large (n_tokens, heads)");
+  return hip_status(spade::launch_cache_append(dc, db, c->d, r, k, k_stride, v, v_stride, q, q_stride,
+                                               Hq, q_out, stream),
+                    "cache append launch");
+}
+
+spade_status spade_cache_read(const spade_cache* c, const spade_batch* b, int64_t N, void* k, void* v,
+                              hipStream_t stream) {
+  spade::DevCache dc;
+  spade::DevBatch db;
+  spade_status st = check_cache(c, &dc);
+  if (st == SPADE_OK) st = check_batch(b, &db);
+  if (st != SPADE_OK) return st;
+  if (N < 0 || N > (int64_t(1) << 31))
+    return fail(SPADE_ERR_INVALID_ARG, "N=%lld must lie in [0, 2^31]", (long long)N);
+  if (b->B == 0 || N == 0) return SPADE_OK;
+  st = check_cache_pointers(dc, true, false);
+  if (st != SPADE_OK) return st;
+  if (!k || !v || k == v || !b->table || !b->lens)
+    return fail(SPADE_ERR_INVALID_ARG, "k, v (two tensors), table and lens must be non-null");
+  if (!aligned16(k) || !aligned16(v))
+    return fail(SPADE_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
+  if (int64_t(b->B) * b->max_pages * c->H * 2 > 0x7fffffff)
+    return fail(SPADE_ERR_UNSUPPORTED, "batch too large (B * max_pages * H)");
+  return hip_status(spade::launch_cache_read(dc, db, c->d, N, k, v, stream), "cache read launch");
+}
+
+size_t spade_cache_select_workspace_bytes(const spade_cache* c, const spade_batch* b, int32_t Hq,
+                                          int32_t topk) {
+  spade::DevCache dc;
+  spade::DevBatch db;
+  if (check_cache(c, &dc) != SPADE_OK || check_batch(b, &db) != SPADE_OK ||
+      check_group(Hq, c->H) != SPADE_OK || topk < 1 || b->B == 0 || b->n_tokens == 0 ||
+      b->max_pages > spade::kCacheMaxPages)
+    return 0;
+  return spade::cache_select_workspace_bytes(dc, db, c->d, Hq, topk);
+}
+
+spade_status spade_cache_select(const spade_cache* c, const spade_batch* b, const void* q, int32_t Hq,
+                                int32_t topk, int32_t sink, int32_t local, int32_t causal,
+                                int32_t* counts, int32_t* indices, void* workspace,
+                                size_t workspace_bytes, hipStream_t stream) {
+  spade::DevCache dc;
+  spade::DevBatch db;
+  spade_status st = check_cache(c, &dc);
+  if (st == SPADE_OK) st = check_batch(b, &db);
+  if (st == SPADE_OK) st = check_group(Hq, c->H);
+  if (st != SPADE_OK) return st;
+  if (causal != 0 && causal != 1)
+    return fail(SPADE_ERR_INVALID_ARG, "causal must be 0 or 1 (got %d)", causal);
+  if (topk < 1 || sink < 0 || local < 0 || int64_t(sink) + local > topk)
+    return fail(SPADE_ERR_INVALID_ARG, "topk=%d >= 1 must hold sink=%d and local=%d pages", topk, sink,
+                local);
+  if (causal && local < 1)
+    return fail(SPADE_ERR_INVALID_ARG,
+                "a causal selection keeps the query's own page: local must be >= 1");
+  if (b->max_pages > spade::kCacheMaxPages)
+    return fail(SPADE_ERR_UNSUPPORTED, "max_pages=%d exceeds the selection limit %d", b->max_pages,
+                spade::kCacheMaxPages);
+  if (b->B == 0 || b->n_tokens == 0) return SPADE_OK;
+  st = check_cache_pointers(dc, false, true);
+  if (st != SPADE_OK) return st;
+  if (!q || !counts || !indices || !b->table || !b->lens || !b->cu)
+    return fail(SPADE_ERR_INVALID_ARG, "q, counts, indices, table, lens and cu must be non-null");
+  if (!aligned16(q)) return fail(SPADE_ERR_INVALID_ARG, "q must be 16-byte aligned");
+  const size_t need = spade::cache_select_workspace_bytes(dc, db, c->d, Hq, topk);
+  if (workspace_bytes < need || (need > 0 && (workspace == nullptr || !aligned16(workspace))))
+    return fail(SPADE_ERR_WORKSPACE, "16-byte aligned workspace of %zu bytes needed, %zu given", need,
+                workspace_bytes);
+  const spade::CacheSelect p = {q, Hq, topk, sink, local, causal != 0, counts, indices};
+  return hip_status(spade::launch_cache_select(dc, db, c->d, p, workspace, stream),
+                    "cache select launch");
+}
+
+size_t spade_cache_attn_workspace_bytes(const spade_cache* c, const spade_batch* b, int32_t Hq,
+                                        int32_t topk) {
+  spade::DevCache dc;
+  spade::DevBatch db;
+  if (check_cache(c, &dc) != SPADE_OK || check_batch(b, &db) != SPADE_OK ||
+      check_group(Hq, c->H) != SPADE_OK || topk < 0 || b->B == 0 || b->n_tokens == 0)
+    return 0;
+  return spade::cache_attn_workspace_bytes(dc, db, c->d, Hq, topk);
+}
+
+spade_status spade_cache_attn(const spade_cache* c, const spade_batch* b, const void* q, int32_t Hq,
+                              const int32_t* counts, const int32_t* indices, int32_t topk,
+                              int32_t causal, double scale, void* o, float* lse, void* workspace,
+                              size_t workspace_bytes, hipStream_t stream) {
+  spade::DevCache dc;
+  spade::DevBatch db;
+  spade_status st = check_cache(c, &dc);
+  if (st == SPADE_OK) st = check_batch(b, &db);
+  if (st == SPADE_OK) st = check_group(Hq, c->H);
+  if (st != SPADE_OK) return st;
+  if (causal != 0 && causal != 1)
+    return fail(SPADE_ERR_INVALID_ARG, "causal must be 0 or 1 (got %d)", causal);
+  if (!(scale >= 1e-30 && scale <= 1e30))
+    return fail(SPADE_ERR_INVALID_ARG, "scale must lie in [1e-30, 1e30] (got %g)", scale);
+  const bool empty = b->B == 0 || b->n_tokens == 0;  // pointers are then not read
+  if (!empty && (counts != nullptr) != (topk > 0))
+    return fail(SPADE_ERR_INVALID_ARG, "topk=%d: the lists' row length with lists, 0 without", topk);
+  if (!empty && (counts == nullptr) != (indices == nullptr))
+    return fail(SPADE_ERR_INVALID_ARG, "counts and indices come together");
+  if (topk < 0) return fail(SPADE_ERR_INVALID_ARG, "topk=%d must be >= 0", topk);
+  if (topk > 0 && b->max_pages > spade::kCacheMaxPages)
+    return fail(SPADE_ERR_UNSUPPORTED, "max_pages=%d exceeds the limit %d of attention with lists",
+                b->max_pages, spade::kCacheMaxPages);
+  if (int64_t(b->max_pages) * c->page > (int64_t(1) << 30))
+    return fail(SPADE_ERR_UNSUPPORTED, "max_pages=%d pages of %d tokens exceed 2^30 tokens", b->max_pages,
+                c->page);
+  if (empty) return SPADE_OK;
+  st = check_cache_pointers(dc, true, false);
+  if (st != SPADE_OK) return st;
+  if (!q || !o || !b->table || !b->lens || !b->cu)
+    return fail(SPADE_ERR_INVALID_ARG, "q, o, table, lens and cu must be non-null");
+  if (!aligned16(q) || !aligned16(o))
+    return fail(SPADE_ERR_INVALID_ARG, "q and o must be 16-byte aligned");
+  if (q == o) return fail(SPADE_ERR_INVALID_ARG, "q and o must not alias");
+  const size_t need = spade::cache_attn_workspace_bytes(dc, db, c->d, Hq, topk);
+  if (workspace_bytes < need || (need > 0 && (workspace == nullptr || !aligned16(workspace))))
+    return fail(SPADE_ERR_WORKSPACE, "16-byte aligned workspace of %zu bytes needed, %zu given", need,
+                workspace_bytes);
+  const spade::CacheAttn p = {q, Hq, topk, counts, indices, float(scale), causal != 0, o, lse};
+  return hip_status(spade::launch_cache_attn(dc, db, c->d, p, workspace, stream),
+                    "cache attention launch");
 }
 
 }  // extern "C"

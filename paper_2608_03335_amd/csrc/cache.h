@@ -1,0 +1,149 @@
+// Paged key/value cache (gfx950): the page layout and what its kernels share.
+//
+// A page holds P tokens of every K/V head (P a multiple of 32), laid out as the matrix
+// instructions read it, so that every wave load of the attention is one contiguous piece
+// and needs no transpose:
+//   K, bf16: [tile of 16 tokens][d / 32][g: 4][m: 16][8 channels], the A operand of
+//            mfma 16x16x32: token 16 tile + m, channel 32 s + 8 g + j; 1 KB a load.
+//   V, bf16: [block of 32 tokens][d / 16][g: 4][m: 16][8 tokens], the A operand of
+//            O^T = V^T P^T: channel 16 ct + m, tokens 4 g + {0..3} and 16 + 4 g + {0..3}:
+//            those whose scores the lane holds after the K product, so P needs no shuffle.
+//   4 bits:  e2m1 values (0, .5, 1, 1.5, 2, 3, 4, 6 with sign), one power of two for each
+//            32 channels of a token, stored as its exponent + 127.
+//   K, 4 bit: [tile][g][m][d / 4 channels], channel (d / 4) g + i: at d = 128 a lane's 16
+//            bytes are one scale group. Scales [tile][d / 32][m].
+//   V, 4 bit: [block][d / 64][g][m][4 column tiles][8 tokens]. Scales [block][g][d / 32][8
+//            tokens], the lane's eight in one piece.
+//   mean:    bf16 [page][H][d], the mean of the page's stored keys.
+#pragma once
+
+#include "spade_internal.h"
+
+namespace spade {
+
+struct DevCache {
+  int H, page, n_pages;
+  bool fp4;
+  void* k;
+  void* v;
+  uint8_t* ks;
+  uint8_t* vs;
+  void* mean;
+};
+
+struct DevBatch {
+  int B, max_pages, n_tokens;
+  const int* table;
+  const int* lens;
+  const int* cu;
+};
+
+struct DevRope {
+  const float* cos;
+  const float* sin;
+  const int* pos;
+  int n_pos, rot, interleaved;
+};
+
+hipError_t launch_cache_append(const DevCache& c, const DevBatch& b, int d, const DevRope& r,
+                               const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                               const void* q, int64_t q_stride, int Hq, void* q_out,
+                               hipStream_t s);
+hipError_t launch_cache_read(const DevCache& c, const DevBatch& b, int d, int64_t N, void* k,
+                             void* v, hipStream_t s);
+
+struct CacheSelect {
+  const void* q;
+  int Hq, topk, sink, local;
+  bool causal;
+  int* counts;
+  int* indices;
+};
+size_t cache_select_workspace_bytes(const DevCache& c, const DevBatch& b, int d, int Hq, int topk);
+hipError_t launch_cache_select(const DevCache& c, const DevBatch& b, int d, const CacheSelect& p,
+                               void* ws, hipStream_t s);
+
+struct CacheAttn {
+  const void* q;
+  int Hq, topk;         // topk 0: no lists, every visible token
+  const int* counts;
+  const int* indices;
+  float scale;
+  bool causal;
+  void* o;
+  float* lse;
+};
+size_t cache_attn_workspace_bytes(const DevCache& c, const DevBatch& b, int d, int Hq, int topk);
+hipError_t launch_cache_attn(const DevCache& c, const DevBatch& b, int d, const CacheAttn& p,
+                             void* ws, hipStream_t s);
+
+constexpr int kCacheMaxPages = 16384;  // pages of a sequence that lists can name (LDS)
+constexpr int kCacheMaxGroup = 128;    // query heads per K/V head
+
+#ifdef __HIPCC__
+typedef __bf16 cbf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 cbf16x8 __attribute__((ext_vector_type(8)));
+typedef float cf32x4 __attribute__((ext_vector_type(4)));
+typedef float cf32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t cu32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t cu32x2 __attribute__((ext_vector_type(2)));
+
+// Work items cut from a batch: sequence b's new tokens cu[b]..cu[b+1]-1 fill at most
+// floor(cu[b+1] / unit) - floor(cu[b] / unit) + extra items, a sum that telescopes, so
+// item ranges need no scan over the sequences and the host knows their total.
+struct SeqItem {
+  int b;      // -1: no such item
+  int first;  // index of the item inside the sequence
+  int t0, n;  // the sequence's new tokens
+};
+
+__host__ __device__ inline int64_t item_base(int tokens, int b, int unit, int extra) {
+  return int64_t(tokens) / unit + int64_t(extra) * b;
+}
+
+// Finds the sequence of a work item: every thread of the block tests some sequences, so
+// the search costs one load, not log2(B) of them. All threads of the block must call.
+// Offsets that do not ascend cannot lead out of the batch's arrays: an item then belongs
+// to one of the sequences that claim it, or to none.
+__device__ __forceinline__ SeqItem find_item(const DevBatch& bt, int64_t item, int unit, int extra,
+                                             int threads) {
+  __shared__ int hit;
+  if (threadIdx.x == 0) hit = -1;
+  __syncthreads();
+  for (int b = threadIdx.x; b < bt.B; b += threads) {
+    const int lo = min(max(bt.cu[b], 0), bt.n_tokens);
+    const int hi = min(max(bt.cu[b + 1], 0), bt.n_tokens);
+    if (hi > lo && item_base(lo, b, unit, extra) <= item && item < item_base(hi, b + 1, unit, extra))
+      hit = b;
+  }
+  __syncthreads();
+  SeqItem r;
+  r.b = hit;
+  r.first = r.t0 = r.n = 0;
+  if (r.b >= 0) {
+    r.t0 = min(max(bt.cu[r.b], 0), bt.n_tokens);
+    r.n = min(max(bt.cu[r.b + 1], 0), bt.n_tokens) - r.t0;
+    r.first = int(item - item_base(r.t0, r.b, unit, extra));
+  }
+  return r;
+}
+
+// 2^(code - 127); code 255, the mark of a group that held a NaN or an infinity, gives an
+// infinity, and the group's values are stored as 0: 0 * inf is NaN wherever it is used.
+__device__ __forceinline__ float scale_of(uint32_t code) { return __uint_as_float(code << 23); }
+
+// bf16 pair from byte BYTE of x, times scale (a power of two: exact)
+template <int BYTE>
+__device__ __forceinline__ cbf16x2 fp4_pair(uint32_t x, float scale) {
+  return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, scale, BYTE);
+}
+
+// the eight values of a dword
+__device__ __forceinline__ cbf16x8 fp4_eight(uint32_t x, float scale) {
+  const cbf16x2 a = fp4_pair<0>(x, scale), b = fp4_pair<1>(x, scale), c = fp4_pair<2>(x, scale),
+                d = fp4_pair<3>(x, scale);
+  return cbf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+#endif
+
+}  // namespace spade

@@ -361,3 +361,135 @@ class SweepPath:
             self.group_attend(c, v, stream)
             self.group_restore(c, heads, v, stream)
         return self.O
+
+
+def grid_rope(T: int, Hs: int, Ws: int, d: int, theta: float = 10000.0, device="cuda"):
+    """Rotation tables (cos, sin), fp32 [T*Hs*Ws, d/2], of a latent grid: the d/2 pairs are
+    shared out over (t, y, x), two of six parts each (t takes what does not divide), and
+    a pair's angle is its coordinate times a power of 1/theta. Row n is raster token n, so
+    a token's raster number is its position. Angles are fp64."""
+    half = d // 2
+    parts = (half - 2 * (half // 3), half // 3, half // 3)
+    n = torch.arange(T * Hs * Ws)
+    place = (n // (Hs * Ws), n // Ws % Hs, n % Ws)
+    angle = torch.cat([p[:, None].double() * theta ** (-torch.arange(m, dtype=torch.float64) / m)
+                       for p, m in zip(place, parts)], 1)
+    return angle.cos().float().to(device), angle.sin().float().to(device)
+
+
+class CachePath:
+    """Attention of a stream: B sequences whose keys and values live in one paged cache.
+
+    Each step takes the new tokens of all sequences: `plan(new)` reserves their pages and
+    writes the batch's offsets (host work and small copies), `run(q, k, v)` issues append,
+    selection (topk > 0) and attention on one stream, with no host sync. A captured graph
+    of `run` serves every later plan with the same number of new tokens and pages enough,
+    since all buffers stay where they are. Pages go back to the pool by `release(b)`;
+    `rewind(b, length)` drops a sequence's last tokens (their pages stay reserved).
+
+    rope: None or (cos, sin) tables; positions are the tokens' places in their sequences
+    unless `run` is given others (raster numbers of a `grid_rope` table)."""
+
+    def __init__(self, B, Hq, H, d, n_pages, max_pages, max_tokens, page=64, fp4=False, topk=0,
+                 sink=0, local=1, causal=True, scale=None, rope=None, interleaved=False,
+                 device="cuda"):
+        self.B, self.Hq, self.H, self.d, self.page = B, Hq, H, d, page
+        self.topk, self.sink, self.local, self.causal = topk, sink, local, causal
+        self.scale = 1.0 / math.sqrt(d) if scale is None else scale
+        self.rope_tables, self.interleaved = rope, interleaved
+        dev = self.device = torch.device(device)
+        e = lambda *s, dt=torch.bfloat16: torch.empty(s, dtype=dt, device=dev)  # noqa: E731
+        fmt = S.SPADE_CACHE_FP4 if fp4 else S.SPADE_CACHE_BF16
+        rows, dt = (d // 2, torch.uint8) if fp4 else (d, torch.bfloat16)
+        self.k, self.v = e(n_pages, H, page, rows, dt=dt), e(n_pages, H, page, rows, dt=dt)
+        self.k_mean = e(n_pages, H, d)
+        self.k_scale = e(n_pages, H, page, d // 32, dt=torch.uint8) if fp4 else None
+        self.v_scale = e(n_pages, H, page, d // 32, dt=torch.uint8) if fp4 else None
+        self.cache = S.cache(fmt, H, d, page, self.k, self.v, self.k_mean, self.k_scale, self.v_scale)
+        self.table = torch.zeros(B, max_pages, dtype=torch.int32, device=dev)
+        self.lens = torch.zeros(B, dtype=torch.int32, device=dev)
+        self.cu = torch.zeros(B + 1, dtype=torch.int32, device=dev)
+        self.max_pages, self.max_tokens = max_pages, max_tokens
+        self.free = list(range(n_pages - 1, -1, -1))
+        self.pages = [[] for _ in range(B)]
+        self.length = [0] * B
+        self.n_tokens = 0
+        self.q = e(max_tokens, Hq, d)
+        self.counts = e(max_tokens, H, dt=torch.int32) if topk else None
+        self.indices = e(max_tokens, H, topk, dt=torch.int32) if topk else None
+        # fewer rows are split over more workgroups: room for every number of new tokens
+        need = 0
+        for n in range(1, max_tokens + 1):
+            b = S.batch(self.table, self.lens, self.cu, n)
+            need = max(need, S.spade_cache_attn_workspace_bytes(self.cache, b, Hq, topk),
+                       S.spade_cache_select_workspace_bytes(self.cache, b, Hq, topk) if topk else 0)
+        self.workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+
+    def plan(self, new):
+        """new: tokens that every sequence gets next. Raises without changing anything when
+        pages or rows are short."""
+        new = [int(n) for n in new]
+        if len(new) != self.B or any(n < 0 for n in new):
+            raise ValueError(f"new must hold {self.B} numbers >= 0")
+        if sum(new) > self.max_tokens:
+            raise ValueError(f"{sum(new)} new tokens, room for {self.max_tokens}")
+        want = [max(-(-(L + n) // self.page) - len(p), 0)
+                for L, n, p in zip(self.length, new, self.pages)]
+        if any(len(p) + w > self.max_pages for p, w in zip(self.pages, want)):
+            raise ValueError(f"a sequence would need more than max_pages={self.max_pages} pages")
+        if sum(want) > len(self.free):
+            raise ValueError(f"{sum(want)} pages needed, {len(self.free)} free")
+        cu = [0]
+        for b, (n, w) in enumerate(zip(new, want)):
+            if w:
+                at = len(self.pages[b])
+                self.pages[b] += [self.free.pop() for _ in range(w)]
+                self.table[b, at:at + w] = torch.tensor(self.pages[b][at:], dtype=torch.int32)
+            self.length[b] += n
+            cu.append(cu[-1] + n)
+        self.n_tokens = cu[-1]
+        self.lens.copy_(torch.tensor(self.length, dtype=torch.int32))
+        self.cu.copy_(torch.tensor(cu, dtype=torch.int32))
+
+    def rewind(self, b: int, length: int):
+        """Sequence b keeps its first `length` tokens."""
+        if not 0 <= length <= self.length[b]:
+            raise ValueError(f"length must lie in [0, {self.length[b]}]")
+        self.length[b] = int(length)
+
+    def release(self, b: int):
+        """Sequence b starts anew; its pages return to the pool."""
+        self.free += reversed(self.pages[b])
+        self.pages[b] = []
+        self.length[b] = 0
+
+    def batch(self):
+        return S.batch(self.table, self.lens, self.cu, self.n_tokens)
+
+    def run(self, q, k, v, out=None, lse=None, pos=None, stream=None):
+        """q [n, Hq, d], k, v [n, H, d], bf16, the planned tokens in sequence order -> [n, Hq, d]."""
+        n, b = self.n_tokens, self.batch()
+        if out is None:
+            out = torch.empty(n, self.Hq, self.d, dtype=torch.bfloat16, device=self.device)
+        rope = None
+        if self.rope_tables is not None:
+            rope = S.rope(*self.rope_tables, pos, interleaved=self.interleaved)
+        qr = self.q[:n]
+        S.spade_cache_append(self.cache, b, k, v, q, qr, rope, stream=stream)
+        counts = indices = None
+        if self.topk:
+            counts, indices = self.counts[:n], self.indices[:n]
+            S.spade_cache_select(self.cache, b, qr, self.topk, counts, indices, causal=self.causal,
+                                 sink=self.sink, local=self.local, workspace=self.workspace,
+                                 stream=stream)
+        S.spade_cache_attn(self.cache, b, qr, self.scale, out, lse, counts, indices,
+                           causal=self.causal, workspace=self.workspace, stream=stream)
+        return out
+
+    def read(self, N=None, stream=None):
+        """Keys and values of all sequences as raster tensors [B, H, N, d], zero behind a sequence."""
+        N = max(self.length) if N is None else N
+        k = torch.zeros(self.B, self.H, N, self.d, dtype=torch.bfloat16, device=self.device)
+        v = torch.zeros_like(k)
+        S.spade_cache_read(self.cache, self.batch(), k, v, stream=stream)
+        return k, v

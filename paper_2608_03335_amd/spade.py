@@ -26,6 +26,7 @@ SPADE_TOPK, SPADE_TOPP = 0, 1
 SPADE_EST_MEAN, SPADE_EST_DSA, SPADE_EST_DSA2 = 0, 1, 2
 SPADE_INTRA_NONE, SPADE_INTRA_THRESHOLD, SPADE_INTRA_TOPK = 0, 1, 2
 SPADE_TASK_T2V, SPADE_TASK_I2V = 0, 1
+SPADE_CACHE_BF16, SPADE_CACHE_FP4 = 0, 1
 SPADE_LIST_BAD_COUNT, SPADE_LIST_BAD_INDEX, SPADE_LIST_NOT_ASCENDING = 1, 2, 4
 
 EXPORTED = ("spade_block_reorder", "spade_summarize", "spade_block_summarize",
@@ -35,7 +36,9 @@ EXPORTED = ("spade_block_reorder", "spade_summarize", "spade_block_summarize",
             "spade_policy_dense", "spade_policy_split", "spade_attn_workspace_bytes",
             "spade_block_sparse_attn", "spade_sparse_attn_raster",
             "spade_sparse_attn_raster_multi", "spade_sparse_attn_raster_noalloc",
-            "spade_validate_lists", "spade_status_string",
+            "spade_validate_lists", "spade_cache_append", "spade_cache_read",
+            "spade_cache_select_workspace_bytes", "spade_cache_attn_workspace_bytes",
+            "spade_cache_select", "spade_cache_attn", "spade_status_string",
             "spade_last_error")
 MAX_HEAD_LIST = 64
 
@@ -98,6 +101,7 @@ def lib() -> ctypes.CDLL:
                                "`python -m paper_2608_03335_amd.build_lib`")
         L = ctypes.CDLL(_LIB_PATH)
         vp, i32, f64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_double, ctypes.c_size_t
+        i64, C, Bt = ctypes.c_int64, ctypes.POINTER(spade_cache), ctypes.POINTER(spade_batch)
         G = ctypes.POINTER(spade_geom)
         sig = {
             "spade_block_reorder": (i32, [G, vp, vp, i32, i32, ctypes.POINTER(i32), i32, vp]),
@@ -125,6 +129,13 @@ def lib() -> ctypes.CDLL:
             "spade_sparse_attn_raster_multi": (i32, [G, i32, ctypes.POINTER(spade_head_lists), vp,
                                                      vp, vp, f64, vp, vp, vp, sz, vp]),
             "spade_validate_lists": (i32, [G, vp, vp, vp, vp]),
+            "spade_cache_append": (i32, [C, Bt, vp, i64, vp, i64, vp, i64, i32, vp,
+                                         ctypes.POINTER(spade_rope), vp]),
+            "spade_cache_read": (i32, [C, Bt, i64, vp, vp, vp]),
+            "spade_cache_select_workspace_bytes": (sz, [C, Bt, i32, i32]),
+            "spade_cache_attn_workspace_bytes": (sz, [C, Bt, i32, i32]),
+            "spade_cache_select": (i32, [C, Bt, vp, i32, i32, i32, i32, i32, vp, vp, vp, sz, vp]),
+            "spade_cache_attn": (i32, [C, Bt, vp, i32, vp, vp, i32, i32, f64, vp, vp, vp, sz, vp]),
             "spade_status_string": (ctypes.c_char_p, [i32]),
             "spade_last_error": (ctypes.c_char_p, []),
         }
@@ -512,3 +523,231 @@ def spade_sparse_attn_raster_noalloc(g: spade_geom, q, k, v, counts, indices, sc
                  a(counts, I32, D.per_block, "counts"), a(indices, I32, D.pairs, "indices"),
                  float(scale), a(o, BF16, D.raster, "o"), a(lse, F32, D.raster_rows, "lse"),
                  stream))
+
+
+# ------------------------------------------------------------- paged key/value cache
+
+class spade_cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("format", "H", "d", "page", "n_pages")] + [
+        (n, ctypes.c_void_p) for n in ("k", "v", "k_mean", "k_scale", "v_scale")]
+
+
+class spade_batch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "max_pages", "n_tokens")] + [
+        (n, ctypes.c_void_p) for n in ("table", "lens", "cu")]
+
+
+class spade_rope(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pos", "rot", "interleaved")] + [
+        (n, ctypes.c_void_p) for n in ("cos", "sin", "pos")]
+
+
+class _CacheArgs(_Args):
+    """_Args of the cache calls: all tensors and structs of a call are on one GPU, and
+    the call is made on it (its current stream unless one is given), whichever device
+    is current. CPU tensors are told apart last, as in _Args."""
+
+    def __init__(self):
+        super().__init__()
+        self.device = None
+
+    def __call__(self, t, dtype, numel, name):
+        p = super().__call__(t, dtype, numel, name)
+        if t is not None:
+            self.on(t.device, name)
+        return p
+
+    def on(self, device, name):
+        if self.device is None:
+            self.device = device
+        elif self.device != device:
+            raise SpadeError(SPADE_ERR_INVALID_ARG,
+                             f"{name} is on {device}, other arguments on {self.device}")
+
+    def tokens(self, t, n, heads, d, name):
+        """(pointer, token stride) of a bf16 [n, heads, d] tensor whose tokens are packed."""
+        if not isinstance(t, torch.Tensor):
+            raise SpadeError(SPADE_ERR_INVALID_ARG, f"{name} must be a torch tensor")
+        if t.dtype is not BF16:
+            raise SpadeError(SPADE_ERR_INVALID_ARG, f"{name} must be {BF16} (got {t.dtype})")
+        if tuple(t.shape) != (n, heads, d):
+            raise SpadeError(SPADE_ERR_INVALID_ARG,
+                             f"{name} must be [{n}, {heads}, {d}] (got {list(t.shape)})")
+        s = t.stride()
+        if n and heads and (s[2] != 1 or (heads > 1 and s[1] != d)):
+            raise SpadeError(SPADE_ERR_INVALID_ARG, f"{name}: a token's heads must be contiguous")
+        self.on(t.device, name)
+        if not t.is_cuda and self.host is None:
+            self.host = name
+        return t.data_ptr() or None, (s[0] if n > 1 else heads * d)
+
+    def run(self, fn, *args):
+        self.ready()
+        if self.device is None or self.device.index == torch.cuda.current_device():
+            return fn(*args[:-1], _s(args[-1]))
+        with torch.cuda.device(self.device):
+            return fn(*args[:-1], _s(args[-1]))
+
+
+def _struct(cls, a, tensors, *fields):
+    """A struct whose tensors are all on a.device; it keeps them alive."""
+    a.ready()
+    x = cls(*fields)
+    x.device, x.tensors = a.device, tensors
+    return x
+
+
+def cache(format: int, H: int, d: int, page: int, k, v, k_mean=None, k_scale=None,
+          v_scale=None) -> spade_cache:
+    """A paged cache over the caller's buffers. The first dimension of every buffer is
+    the page pool; BF16: k, v bf16 with H * page * d elements a page; FP4: uint8 with
+    H * page * d / 2, and the scales uint8 with H * page * d / 32; k_mean bf16 [n_pages, H, d]."""
+    if format not in (SPADE_CACHE_BF16, SPADE_CACHE_FP4):
+        raise SpadeError(SPADE_ERR_INVALID_ARG, f"unknown cache format {format}")
+    if not isinstance(k, torch.Tensor) or k.dim() < 1:
+        raise SpadeError(SPADE_ERR_INVALID_ARG, "k must be a torch tensor")
+    a = _CacheArgs()
+    n = int(k.shape[0])
+    rows = n * int(H) * int(page)
+    fp4 = format == SPADE_CACHE_FP4
+    dt, per = (torch.uint8, d // 2) if fp4 else (BF16, d)
+    if fp4 and (k_scale is None or v_scale is None):
+        raise SpadeError(SPADE_ERR_INVALID_ARG, "a 4-bit cache needs k_scale and v_scale")
+    ptrs = [a(k, dt, rows * per, "k"), a(v, dt, rows * per, "v"),
+            a(k_mean, BF16, n * int(H) * int(d), "k_mean"),
+            a(k_scale, torch.uint8, rows * (d // 32), "k_scale") if fp4 else None,
+            a(v_scale, torch.uint8, rows * (d // 32), "v_scale") if fp4 else None]
+    return _struct(spade_cache, a, (k, v, k_mean, k_scale, v_scale), int(format), int(H), int(d),
+                   int(page), n, *ptrs)
+
+
+def batch(table, lens, cu, n_tokens: int) -> spade_batch:
+    """The sequences of a call: table int32 [B, max_pages], lens int32 [B], cu int32 [B + 1];
+    n_tokens: rows of the call's packed tensors (cu[B] when every row has a sequence)."""
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise SpadeError(SPADE_ERR_INVALID_ARG, "table must be a [B, max_pages] tensor")
+    a = _CacheArgs()
+    B, width = (int(x) for x in table.shape)
+    ptrs = [a(table, I32, None, "table"), a(lens, I32, B, "lens"), a(cu, I32, B + 1, "cu")]
+    return _struct(spade_batch, a, (table, lens, cu), B, width, int(n_tokens), *ptrs)
+
+
+def rope(cos, sin, pos=None, interleaved: bool = False) -> spade_rope:
+    """Rotation tables fp32 [n_pos, rot / 2] and the tokens' rows int32 [n_tokens] (None: their
+    places in their sequences)."""
+    if not isinstance(cos, torch.Tensor) or cos.dim() != 2:
+        raise SpadeError(SPADE_ERR_INVALID_ARG, "cos must be a [n_pos, rot / 2] tensor")
+    a = _CacheArgs()
+    n, half = (int(x) for x in cos.shape)
+    ptrs = [a(cos, F32, None, "cos"), a(sin, F32, n * half, "sin"), a(pos, I32, None, "pos")]
+    x = _struct(spade_rope, a, (cos, sin, pos), n, 2 * half, int(bool(interleaved)), *ptrs)
+    return x
+
+
+def _cache_args(c, b):
+    if not isinstance(c, spade_cache) or not isinstance(b, spade_batch):
+        raise SpadeError(SPADE_ERR_INVALID_ARG, "c must come from cache(), b from batch()")
+    a = _CacheArgs()
+    a.on(c.device, "c")
+    a.on(b.device, "b")
+    return a
+
+
+def _workspace(a, workspace):
+    if workspace is None:
+        return None, 0
+    return (a(workspace, None, None, "workspace"), workspace.numel() * workspace.element_size())
+
+
+def spade_cache_append(c: spade_cache, b: spade_batch, k, v, q=None, q_out=None,
+                       rope: spade_rope | None = None, stream=None):
+    """k, v: bf16 [n_tokens, H, d], q: bf16 [n_tokens, Hq, d] or None; the tokens may be strided
+    (slices of a fused projection). q_out: contiguous, like q."""
+    a = _cache_args(c, b)
+    n = b.n_tokens
+    kp, ks = a.tokens(k, n, c.H, c.d, "k")
+    vp, vs = a.tokens(v, n, c.H, c.d, "v")
+    qp, qs, Hq, op = None, 0, 0, None
+    if (q is None) != (q_out is None):
+        raise SpadeError(SPADE_ERR_INVALID_ARG, "q and q_out come together")
+    if q is not None:
+        Hq = int(q.shape[1]) if isinstance(q, torch.Tensor) and q.dim() == 3 else 0
+        qp, qs = a.tokens(q, n, Hq, c.d, "q")
+        op = a(q_out, BF16, n * Hq * c.d, "q_out")
+    if rope is not None:
+        if not isinstance(rope, spade_rope):
+            raise SpadeError(SPADE_ERR_INVALID_ARG, "rope must come from rope()")
+        a.on(rope.device, "rope")
+        pos = rope.tensors[2]
+        if pos is not None and pos.numel() < n:
+            raise SpadeError(SPADE_ERR_INVALID_ARG,
+                             f"pos holds {pos.numel()} elements, {n} needed")
+    _check(a.run(lib().spade_cache_append, ctypes.byref(c), ctypes.byref(b), kp, ks, vp, vs, qp, qs,
+                 Hq, op, None if rope is None else ctypes.byref(rope), stream))
+
+
+def spade_cache_read(c: spade_cache, b: spade_batch, k, v, stream=None):
+    """k, v: out, bf16 [B, H, N, d] raster tensors."""
+    a = _cache_args(c, b)
+    if not isinstance(k, torch.Tensor) or k.dim() != 4:
+        raise SpadeError(SPADE_ERR_INVALID_ARG, "k must be a [B, H, N, d] tensor")
+    B, H, N, d = (int(x) for x in k.shape)
+    if (B, H, d) != (b.B, c.H, c.d):
+        raise SpadeError(SPADE_ERR_INVALID_ARG,
+                         f"k must be [{b.B}, {c.H}, N, {c.d}] (got {list(k.shape)})")
+    kp = a(k, BF16, None, "k")
+    vp = a(v, BF16, k.numel(), "v")
+    _check(a.run(lib().spade_cache_read, ctypes.byref(c), ctypes.byref(b), N, kp, vp, stream))
+
+
+def spade_cache_select_workspace_bytes(c: spade_cache, b: spade_batch, Hq: int, topk: int) -> int:
+    return int(lib().spade_cache_select_workspace_bytes(ctypes.byref(c), ctypes.byref(b), int(Hq),
+                                                        int(topk)))
+
+
+def spade_cache_attn_workspace_bytes(c: spade_cache, b: spade_batch, Hq: int, topk: int = 0) -> int:
+    return int(lib().spade_cache_attn_workspace_bytes(ctypes.byref(c), ctypes.byref(b), int(Hq),
+                                                      int(topk)))
+
+
+def _queries(a, b, c, q, name="q"):
+    """(pointer, Hq) of a contiguous bf16 [n_tokens, Hq, d] tensor."""
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or tuple(q.shape[::2]) != (b.n_tokens, c.d):
+        raise SpadeError(SPADE_ERR_INVALID_ARG, f"{name} must be [{b.n_tokens}, Hq, {c.d}]")
+    return a(q, BF16, None, name), int(q.shape[1])
+
+
+def spade_cache_select(c: spade_cache, b: spade_batch, q, topk: int, counts, indices,
+                       causal: bool = True, sink: int = 0, local: int = 1, workspace=None,
+                       stream=None):
+    """q: bf16 [n_tokens, Hq, d]; counts: int32 [n_tokens, H]; indices: int32 [n_tokens, H, topk]."""
+    a = _cache_args(c, b)
+    qp, Hq = _queries(a, b, c, q)
+    rows = b.n_tokens * c.H
+    ws, nbytes = _workspace(a, workspace)
+    _check(a.run(lib().spade_cache_select, ctypes.byref(c), ctypes.byref(b), qp, Hq, int(topk),
+                 int(sink), int(local), int(bool(causal)), a(counts, I32, rows, "counts"),
+                 a(indices, I32, rows * max(int(topk), 0), "indices"), ws, nbytes, stream))
+
+
+def spade_cache_attn(c: spade_cache, b: spade_batch, q, scale: float, o, lse=None, counts=None,
+                     indices=None, causal: bool = True, workspace=None, stream=None):
+    """q, o: bf16 [n_tokens, Hq, d]; counts, indices: int32 [n_tokens, H], [n_tokens, H, topk], or
+    None for all visible tokens; lse: fp32 [n_tokens, Hq] or None."""
+    a = _cache_args(c, b)
+    qp, Hq = _queries(a, b, c, q)
+    rows = b.n_tokens * c.H
+    topk = 0
+    if (counts is None) != (indices is None):
+        raise SpadeError(SPADE_ERR_INVALID_ARG, "counts and indices come together")
+    if indices is not None:
+        if not isinstance(indices, torch.Tensor) or indices.dim() != 3 or (
+                tuple(indices.shape[:2]) != (b.n_tokens, c.H)):
+            raise SpadeError(SPADE_ERR_INVALID_ARG,
+                             f"indices must be [{b.n_tokens}, {c.H}, topk]")
+        topk = int(indices.shape[2])
+    ws, nbytes = _workspace(a, workspace)
+    _check(a.run(lib().spade_cache_attn, ctypes.byref(c), ctypes.byref(b), qp, Hq,
+                 a(counts, I32, rows, "counts"), a(indices, I32, None, "indices"), topk,
+                 int(bool(causal)), float(scale), a(o, BF16, b.n_tokens * Hq * c.d, "o"),
+                 a(lse, F32, b.n_tokens * Hq, "lse"), ws, nbytes, stream))

@@ -1,0 +1,193 @@
+"""The cache calls together, as a layer uses them: CachePath over a stream of tokens, its
+captured graph, several streams at once, and the raster attention fed from the cache."""
+import math
+
+import pytest
+import torch
+
+from paper_2608_03335_amd import spade as S
+from paper_2608_03335_amd.pipeline import CachePath, grid_rope
+
+from . import _cache as C
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _say(*a):
+    print(*a, flush=True)
+
+
+class Mirror:
+    """The same stream in 64 bits on the CPU."""
+
+    def __init__(self, p, cos, sin, fp4):
+        self.p, self.cos, self.sin, self.fp4 = p, cos, sin, fp4
+        self.k = [torch.zeros(0, p.H, p.d, dtype=torch.float64) for _ in range(p.B)]
+        self.v = [torch.zeros(0, p.H, p.d, dtype=torch.float64) for _ in range(p.B)]
+
+    def step(self, new, q, k, v):
+        p, t0, out = self.p, 0, []
+        for b, n in enumerate(new):
+            L0 = len(self.k[b])
+            at = slice(L0, L0 + n)
+            turn = lambda x: C.rotate(x, self.cos[at], self.sin[at], p.interleaved)  # noqa: E731
+            rows = slice(t0, t0 + n)
+            self.k[b] = torch.cat([self.k[b], C.stored(turn(k[rows]), self.fp4)])
+            self.v[b] = torch.cat([self.v[b], C.stored(v[rows], self.fp4)])
+            seen = C.seen_by(L0 + n, n, p.causal)
+            qr = turn(q[rows])
+            lists = C.select(qr, C.page_means(self.k[b], p.page), seen, p.page, p.topk, p.sink,
+                             p.local) if p.topk and n else None
+            if n:
+                out.append(C.attend(qr, self.k[b], self.v[b], seen, lists, p.page, p.scale))
+            t0 += n
+        return [torch.cat(x) for x in zip(*out)]
+
+
+@pytest.mark.parametrize("fp4,topk,causal,inter", [(False, 3, True, False), (True, 3, True, True),
+                                                   (False, 0, True, True), (True, 4, False, False)])
+def test_stream(fp4, topk, causal, inter):
+    B, Hq, H, d, page = 3, 4, 2, 64, 32
+    _say("stream", fp4, topk, causal)
+    cos, sin = grid_rope(6, 7, 9, d, device="cpu")
+    p = CachePath(B, Hq, H, d, n_pages=40, max_pages=11, max_tokens=120, page=page, fp4=fp4, topk=topk,
+                  sink=1, local=1, causal=causal, rope=(cos.to(DEV), sin.to(DEV)), interleaved=inter,
+                  device=DEV)
+    ref = Mirror(p, cos, sin, fp4)
+    gen = torch.Generator().manual_seed(1)
+    for new in ([50, 3, 0], [1, 1, 1], [1, 1, 1], [5, 60, 40], [1, 0, 1], [90, 2, 1]):
+        n = sum(new)
+        q, k, v = (torch.randn(n, h, d, generator=gen).to(torch.bfloat16) for h in (Hq, H, H))
+        p.plan(new)
+        lse = torch.empty(n, Hq, dtype=torch.float32, device=DEV)
+        o = p.run(q.to(DEV), k.to(DEV), v.to(DEV), lse=lse)
+        torch.cuda.synchronize()
+        ro, rl, o_tol, l_tol = ref.step(new, q, k, v)
+        assert bool(((o.cpu().double() - ro).abs() <= o_tol).all())
+        assert bool(((lse.cpu().double() - rl).abs() <= l_tol).all())
+    rk, rv = p.read()
+    for b in range(B):
+        L = p.length[b]
+        assert torch.equal(rk[b, :, :L].cpu().double(), ref.k[b].transpose(0, 1))
+        assert torch.equal(rv[b, :, :L].cpu().double(), ref.v[b].transpose(0, 1))
+        assert bool((rk[b, :, L:] == 0).all())
+
+
+def test_pages_are_reserved_returned_and_refused():
+    p = CachePath(2, 2, 2, 64, n_pages=5, max_pages=4, max_tokens=100, page=32, device=DEV)
+    p.plan([33, 32])
+    assert len(p.free) == 2 and [len(x) for x in p.pages] == [2, 1]
+    for bad in ([1], [-1, 0], [101, 0], [0, 97], [64, 64]):
+        with pytest.raises(ValueError):
+            p.plan(bad)
+    assert p.length == [33, 32] and len(p.free) == 2
+    p.rewind(0, 5)
+    p.plan([20, 1])
+    assert p.length == [25, 33] and len(p.free) == 1
+    with pytest.raises(ValueError):
+        p.rewind(0, 26)
+    p.release(0)
+    assert len(p.free) == 3 and p.length[0] == 0
+    p.plan([0, 0])
+    assert p.run(*(torch.empty(0, 2, 64, dtype=torch.bfloat16, device=DEV) for _ in range(3))).shape == (0, 2, 64)
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+def test_captured_step_serves_later_tokens(fp4):
+    """A graph of one decode step, replayed as the contexts grow, against the eager calls on a
+    second path; eager work and synchronisations lie between the replays."""
+    B, Hq, H, d = 3, 8, 2, 128
+    cos, sin = grid_rope(10, 10, 10, d, device=DEV)
+    make = lambda: CachePath(B, Hq, H, d, n_pages=60, max_pages=16, max_tokens=600, page=64, fp4=fp4,  # noqa: E731
+                             topk=4, sink=1, local=1, rope=(cos, sin), device=DEV)
+    a, e = make(), make()
+    gen = torch.Generator().manual_seed(2)
+    rand = lambda n, h: torch.randn(n, h, d, generator=gen).to(torch.bfloat16).to(DEV)  # noqa: E731
+    first = (rand(600, Hq), rand(600, H), rand(600, H))
+    for p in (a, e):
+        p.plan([100, 180, 320])
+        p.run(*first)
+    q, k, v = rand(B, Hq), rand(B, H), rand(B, H)
+    o = torch.empty(B, Hq, d, dtype=torch.bfloat16, device=DEV)
+    a.plan([1] * B)
+    e.plan([1] * B)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        a.run(q, k, v, out=o)
+    torch.cuda.current_stream().wait_stream(side)
+    want = e.run(q, k, v)
+    torch.cuda.synchronize()
+    assert torch.equal(o, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.run(q, k, v, out=o)
+    for step in range(5):
+        nq, nk, nv = rand(B, Hq), rand(B, H), rand(B, H)
+        a.plan([1] * B)
+        e.plan([1] * B)
+        q.copy_(nq), k.copy_(nk), v.copy_(nv)
+        o.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = e.run(nq, nk, nv)
+        torch.cuda.synchronize()
+        assert torch.equal(o, want), step
+        _ = (nq.float() @ nq.float().transpose(1, 2)).sum()
+    ka, va = a.read()
+    ke, ve = e.read()
+    assert torch.equal(ka, ke) and torch.equal(va, ve)
+
+
+def test_two_streams_at_once():
+    """Two paths with their own buffers on two streams: the same bits as one after the other."""
+    B, Hq, H, d = 2, 8, 4, 128
+    gen = torch.Generator().manual_seed(3)
+    rand = lambda n, h: torch.randn(n, h, d, generator=gen).to(torch.bfloat16).to(DEV)  # noqa: E731
+    data = [(rand(900, Hq), rand(900, H), rand(900, H)) for _ in range(2)]
+    paths = [CachePath(B, Hq, H, d, n_pages=40, max_pages=20, max_tokens=900, page=64, topk=3, sink=1,
+                       local=1, fp4=bool(i), device=DEV) for i in range(2)]
+    want = []
+    for p, x in zip(paths, data):
+        p.plan([500, 400])
+        want.append(p.run(*x))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.full_like(w, float("nan")) for w in want]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for p, x, s, o in zip(paths, data, streams, outs):
+            p.run(*x, out=o, stream=s)
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert torch.equal(o, w)
+
+
+def test_raster_attention_from_the_cache():
+    """A 4-bit cache read back as raster tensors feeds the block-sparse attention: with every
+    block kept it gives what the cache attention gives over all tokens, in both allowances."""
+    T, Hs, Ws, H, d = 3, 8, 10, 2, 64
+    N = T * Hs * Ws
+    cos, sin = grid_rope(T, Hs, Ws, d, device=DEV)
+    p = CachePath(1, H, H, d, n_pages=10, max_pages=8, max_tokens=N, page=32, fp4=True, causal=False,
+                  rope=(cos, sin), interleaved=True, device=DEV)
+    gen = torch.Generator().manual_seed(4)
+    q, k, v = (torch.randn(N, H, d, generator=gen).to(torch.bfloat16) for _ in range(3))
+    p.plan([N])
+    o = p.run(q.to(DEV), k.to(DEV), v.to(DEV))
+    rk, rv = p.read()
+    g = S.geom(1, H, d, T, Hs, Ws, 1, 4, 5)
+    counts = torch.full((1, H, g.NB), g.NB, dtype=torch.int32, device=DEV)
+    idx = torch.arange(g.NB, dtype=torch.int32, device=DEV).repeat(1, H, g.NB, 1).contiguous()
+    qr = p.q[:N].transpose(0, 1)[None].contiguous()
+    out = torch.empty_like(qr)
+    ws = torch.empty(S.spade_attn_workspace_bytes(g), dtype=torch.uint8, device=DEV)
+    S.spade_sparse_attn_raster(g, qr, rk, rv, counts, idx, 1 / math.sqrt(d), out, workspace=ws)
+    torch.cuda.synchronize()
+    toks = [x[0].cpu().double().transpose(0, 1) for x in (rk, rv)]
+    want, _, tol, _ = C.attend(p.q[:N].cpu(), *toks, [N] * N, None, 32, 1 / math.sqrt(d))
+    assert bool(((o.cpu().double() - want).abs() <= tol).all())
+    other = out[0].transpose(0, 1).cpu().double()
+    # the block attention also rounds the weights it sums to bf16: 2^-8 of the value more
+    assert bool(((other - want).abs() <= tol + C.BF16_HALF * want.abs()).all())
