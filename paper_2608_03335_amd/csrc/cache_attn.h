@@ -1,0 +1,49 @@
+// What the two attention kernels of the paged cache share (cache_attn.hip, cache_chunk.hip).
+#pragma once
+
+#include "cache.h"
+
+namespace spade {
+
+struct AttnArgs {
+  DevCache c;
+  DevBatch b;
+  const __bf16* q;
+  const int* counts;
+  const int* indices;
+  int topk, Hq, G;
+  int QT, RT;               // tokens a tile; row tiles a K/V head (G larger than a tile)
+  float scale2;             // logit scale * log2(e)
+  int causal;
+  __bf16* o;
+  float* lse;
+  float* part;              // partial results (splits > 1)
+  int splits;               // most workgroups that share a tile's walk
+};
+
+// Many queries a sequence: tiles of 128 rows that share staged keys (cache_chunk.hip).
+// chunk_items: work items, 0 where the kernel does not serve the call.
+int64_t chunk_items(const DevCache& c, const DevBatch& b, int Hq);
+hipError_t launch_chunk_attn(const AttnArgs& a, int d, hipStream_t s);
+
+#ifdef __HIPCC__
+constexpr float kLn2f = 0.69314718055994530942f;
+constexpr float kNegInf = -__builtin_huge_valf();
+
+// Visible tokens of a sequence's new tokens: token i of n sees first + i * step, clamped.
+struct Seen {
+  int first, step, len;
+  __device__ __forceinline__ int of(int i) const { return min(max(first + i * step, 0), len); }
+};
+__device__ __forceinline__ Seen seen_of(const AttnArgs& a, int b, int n) {
+  const int64_t raw = a.b.lens[b];
+  Seen s;
+  s.len = int(min(max(raw, int64_t(0)), int64_t(a.b.max_pages) * a.c.page));
+  s.step = a.causal;
+  // a context of fewer tokens than are new leaves the first ones nothing to see
+  s.first = a.causal ? int(max(raw - n + 1, int64_t(-(1 << 30)))) : s.len;
+  return s;
+}
+#endif
+
+}  // namespace spade

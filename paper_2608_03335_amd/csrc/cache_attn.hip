@@ -19,9 +19,9 @@
 // Masked places: keys beyond the tile's last visible token are cleared in V as well as in
 // P (their memory may hold anything, NaN among it). A key that some rows of the tile see
 // and others do not can hold a NaN or infinity in V that 0 * x would carry into the rows
-// that must not see it: a wave whose result has a NaN repeats its walk token by token,
-// clearing V for each (`careful`).
-#include "cache.h"
+// that must not see it: a workgroup whose result has a NaN repeats its walk for each token
+// alone, clearing V beyond what that token sees.
+#include "cache_attn.h"
 
 namespace spade {
 namespace {
@@ -29,39 +29,38 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kMaxSplits = 64;
-constexpr float kLn2f = 0.69314718055994530942f;
-constexpr float kNegInf = -__builtin_huge_valf();
-
-struct AttnArgs {
-  DevCache c;
-  DevBatch b;
-  const __bf16* q;
-  const int* counts;
-  const int* indices;
-  int topk, Hq, G, QT, RT;  // QT: tokens a tile; RT: row tiles a K/V head (G > 16)
-  float scale2;             // logit scale * log2(e)
-  int causal;
-  __bf16* o;
-  float* lse;
-  float* part;              // partial results (splits > 1)
-  int splits;
-};
+constexpr int kMinUnits = 16;      // units a split is worth: its start and join cost as much
+constexpr int kTargetWgs = 2048;   // workgroups a call is split into, about
+constexpr float kLazy = 8.0f;      // the running maximum is raised when a row's grew by 2^8
 
 // What a work item covers; the same in the attention and in the join.
 struct Tile {
-  int b, t0, nq;       // sequence, first token, tokens
-  int h, head0, heads; // K/V head, first query head, query heads of the tile
-  int first_seen;      // visible tokens of the tile's first token
-  int step;            // by how much the next token sees more (causal: 1)
-  int len;             // no token sees more than this
-  int pages;           // pages its last token sees
-  int splits;          // workgroups that share its walk
-  __device__ __forceinline__ int seen(int i) const {
-    return min(max(first_seen + i * step, 0), len);
-  }
+  int b, t0, nq;        // sequence, first token, tokens
+  int h, head0, heads;  // K/V head, first query head, query heads of the tile
+  Seen seen;            // of the tile's tokens
+  int pages;            // pages its last token sees
+  int splits;           // workgroups that share its walk
 };
 
+__device__ __forceinline__ int tile_walk(const AttnArgs& a, int pages) {  // pages, at most
+  return a.topk ? int(min(int64_t(a.topk) * a.QT, int64_t(pages))) : pages;
+}
+
 __device__ __forceinline__ bool find_tile(const AttnArgs& a, Tile* t) {
+  // all units of the call, for the splits' size
+  __shared__ unsigned long long total;
+  if (threadIdx.x == 0) total = 0;
+  const int P = a.c.page;
+  if (a.splits > 1) {
+    __syncthreads();
+    unsigned long long mine = 0;
+    for (int b = threadIdx.x; b < a.b.B; b += kThreads) {
+      const int64_t n = int64_t(a.b.cu[b + 1]) - a.b.cu[b];
+      const int64_t len = min(max(int64_t(a.b.lens[b]), int64_t(0)), int64_t(a.b.max_pages) * P);
+      if (n > 0) mine += int64_t((n + a.QT - 1) / a.QT) * tile_walk(a, int((len + P - 1) / P));
+    }
+    if (mine) atomicAdd(&total, mine);
+  }
   const SeqItem it = find_item(a.b, blockIdx.x, a.QT, a.QT > 1, kThreads);
   if (it.b < 0) return false;
   const int skip = it.first * a.QT;
@@ -73,31 +72,24 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& a, Tile* t) {
   const int r0 = (blockIdx.y - t->h * a.RT) * 16;
   t->head0 = t->h * a.G + r0;
   t->heads = min(a.G - r0, 16);
-  const int P = a.c.page;
-  const int64_t raw = a.b.lens[it.b];
-  t->len = int(min(max(raw, int64_t(0)), int64_t(a.b.max_pages) * P));
-  t->step = a.causal;
-  // a context of fewer tokens than are new leaves the first ones nothing to see
-  t->first_seen = a.causal ? int(max(raw - it.n + skip + 1, int64_t(-(1 << 30)))) : t->len;
-  const int most = t->seen(t->nq - 1);
-  t->pages = (most + P - 1) / P;
-  int walk = t->pages;
-  if (a.topk) {  // an upper bound of the union of the lists
-    int64_t sum = 0;
-    for (int i = 0; i < t->nq; ++i) {
-      const int n = a.counts[int64_t(t->t0 + i) * a.c.H + t->h];
-      sum += min(max(n, 0), a.topk);
-    }
-    walk = int(min(sum, int64_t(walk)));
+  t->seen = seen_of(a, it.b, it.n);
+  t->seen.first += skip * t->seen.step;
+  t->pages = (t->seen.of(t->nq - 1) + P - 1) / P;
+  t->splits = 1;
+  if (a.splits > 1) {
+    const int64_t upp = P >> 5, units = tile_walk(a, t->pages) * upp;
+    const int64_t even = (int64_t(total) * upp * gridDim.y + kTargetWgs - 1) / kTargetWgs;
+    const int64_t size = max(even, int64_t(kMinUnits));
+    t->splits = int(min(max((units + size - 1) / size, int64_t(1)), int64_t(a.splits)));
   }
-  const int units = walk * (P >> 5);
-  t->splits = min(max((units + 4 * kWaves - 1) / (4 * kWaves), 1), a.splits);
   return true;
 }
 
-__device__ __forceinline__ float max16(float v) {  // over the lanes of one row
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+__device__ __forceinline__ float max16(float v) {  // over the four lanes of a row
+  const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+  const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
 }
 __device__ __forceinline__ float sum16(float v) {
   v += __shfl_xor(v, 16);
@@ -178,19 +170,19 @@ __device__ __forceinline__ void load_q(const AttnArgs& a, const Tile& t, int lan
   }
 }
 
-// One unit: keys at..at+31 of the sequence. full: every row sees every key. V is cleared from
-// key v_seen on; the rows of lanes without `take` keep what they had.
-template <int D, bool FP4>
+// One unit: keys at..at+31 of the sequence. row_in: the lane's row keeps the page. EDGE: a row
+// sees the keys below row_seen, and V is cleared from key v_seen on.
+template <int D, bool FP4, bool EDGE>
 __device__ __forceinline__ void step_unit(const UnitLoad<D, FP4>& u, Wave<D, FP4>& w, int lane,
                                           float scale2, int at, int row_seen, bool row_in,
-                                          int v_seen, bool full, bool take) {
+                                          int v_seen) {
   constexpr int KK = D / 32, CT = D / 16;
   const int g = lane >> 4;
   cf32x4 s[2] = {};
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int k = 0; k < KK; ++k)
 #pragma unroll
-    for (int k = 0; k < KK; ++k) {
+    for (int i = 0; i < 2; ++i) {
       cbf16x8 f;
       if constexpr (FP4) f = fp4_eight(u.k[(i * KK + k) >> 2][(i * KK + k) & 3], scale_of(u.ks[i]));
       else f = __builtin_bit_cast(cbf16x8, u.k[i * KK + k]);
@@ -199,25 +191,35 @@ __device__ __forceinline__ void step_unit(const UnitLoad<D, FP4>& u, Wave<D, FP4
   float p[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int key = at + (i >> 2) * 16 + g * 4 + (i & 3);
-    p[i] = s[i >> 2][i & 3] * scale2;
-    if (!full) p[i] = row_in && key < row_seen ? p[i] : kNegInf;
+    p[i] = s[i >> 2][i & 3];
+    if constexpr (EDGE) p[i] = at + (i >> 2) * 16 + g * 4 + (i & 3) < row_seen ? p[i] : kNegInf;
   }
-  float top = p[0];
+  float top = fmaxf(p[0], p[1]);
 #pragma unroll
-  for (int i = 1; i < 8; ++i) top = fmaxf(top, p[i]);
-  top = max16(top);
-  const float m = fmaxf(w.m, top);
-  const float base = m == kNegInf ? 0.0f : m;  // no key yet: every p is 2^-inf = 0
-  const float alpha = __builtin_amdgcn_exp2f(w.m - base);
+  for (int i = 2; i < 8; i += 2) top = fmaxf(fmaxf(top, p[i]), p[i + 1]);
+  top = max16(top) * scale2;
+  top = row_in ? top : kNegInf;
+  float m = w.m;
+  if (__any(top > m + kLazy)) {
+    m = top > m + kLazy ? top : m;
+    const float alpha = w.m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(w.m - m);
+#pragma unroll
+    for (int c = 0; c < CT; ++c) w.o[c] *= alpha;
+    w.l *= alpha;
+    w.m = m;
+  }
+  // rows that do not keep the page, or have no key yet: 2^(s - inf) = 0
+  const float bias = row_in && m != kNegInf ? -m : kNegInf;
   float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    p[i] = __builtin_amdgcn_exp2f(p[i] - base);
+    p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[i], scale2, bias));
     sum += p[i];
   }
-  // V^T operands, cleared beyond v_seen
-  const bool edge = at + 32 > v_seen;
+  w.l += sum;
+  auto add = [&](int c, cbf16x8 f, cbf16x8 pf) {
+    w.o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pf, w.o[c], 0, 0, 0);
+  };
   if constexpr (!FP4) {
     cbf16x8 pf;
 #pragma unroll
@@ -225,41 +227,46 @@ __device__ __forceinline__ void step_unit(const UnitLoad<D, FP4>& u, Wave<D, FP4
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
       cbf16x8 f = __builtin_bit_cast(cbf16x8, u.v[c]);
-      if (edge)
+      if constexpr (EDGE)
 #pragma unroll
         for (int i = 0; i < 8; ++i)
           f[i] = at + (i >> 2) * 16 + g * 4 + (i & 3) < v_seen ? f[i] : (__bf16)0.0f;
-      const cf32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pf, w.o[c] * alpha, 0, 0, 0);
-      w.o[c] = take ? x : w.o[c];
+      add(c, f, pf);
     }
   } else {
-    float two[8];
 #pragma unroll
     for (int gr = 0; gr < D / 32; ++gr) {
       cbf16x8 pf;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        two[i] = scale_of((u.vs[gr][i >> 2] >> (8 * (i & 3))) & 255u);
-        if (edge) two[i] = at + (i >> 2) * 16 + g * 4 + (i & 3) < v_seen ? two[i] : 0.0f;
-        pf[i] = (__bf16)(p[i] * two[i]);
+        float two = scale_of((u.vs[gr][i >> 2] >> (8 * (i & 3))) & 255u);
+        if constexpr (EDGE) two = at + (i >> 2) * 16 + g * 4 + (i & 3) < v_seen ? two : 0.0f;
+        pf[i] = (__bf16)(p[i] * two);
       }
 #pragma unroll
       for (int cc = 0; cc < 2; ++cc) {
         const int c = gr * 2 + cc;
-        const cf32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            fp4_eight(u.v[c >> 2][c & 3], 1.0f), pf, w.o[c] * alpha, 0, 0, 0);
-        w.o[c] = take ? x : w.o[c];
+        add(c, fp4_eight(u.v[c >> 2][c & 3], 1.0f), pf);
       }
     }
   }
-  if (take) {
-    w.l = w.l * alpha + sum;
-    w.m = m;
-  }
+}
+
+// Four channels of a finished row.
+template <int D>
+__device__ __forceinline__ void write_row(const AttnArgs& a, const Tile& t, int rq, int gh, int c4,
+                                          cf32x4 x, float top, float sum) {
+  const float inv = top == kNegInf ? 0.0f : 1.0f / sum;
+  const int64_t orow = int64_t(t.t0 + rq) * a.Hq + t.head0 + gh;
+  cu32x2 y;
+  y[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector(cf32x2{x[0] * inv, x[1] * inv}, cbf16x2));
+  y[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(cf32x2{x[2] * inv, x[3] * inv}, cbf16x2));
+  *(cu32x2*)(a.o + orow * D + c4 * 4) = y;
+  if (a.lse && c4 == 0) a.lse[orow] = (top + log2f(sum)) * kLn2f;
 }
 
 template <int D, bool FP4>
-__global__ void __launch_bounds__(kThreads) cache_attn_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) cache_attn_kernel(AttnArgs a) {
   constexpr int CT = D / 16;
   constexpr int OROW = D + 4;  // fp32 row of the waves' merge in LDS
   extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -279,7 +286,7 @@ __global__ void __launch_bounds__(kThreads) cache_attn_kernel(AttnArgs a) {
     for (int i = 0; i < t.nq; ++i) {
       const int64_t row = int64_t(t.t0 + i) * a.c.H + t.h;
       const int n = min(max(a.counts[row], 0), a.topk);
-      const int vis = (t.seen(i) + P - 1) / P;
+      const int vis = (t.seen.of(i) + P - 1) / P;
       for (int k = tid; k < n; k += kThreads) {
         const int j = a.indices[row * a.topk + k];
         if (j >= 0 && j < vis) atomicOr(&list[j], 1u << i);
@@ -307,132 +314,185 @@ __global__ void __launch_bounds__(kThreads) cache_attn_kernel(AttnArgs a) {
   Wave<D, FP4> w;
   load_q(a, t, lane, w);
   const int qi = (lane & 15) / t.heads;  // the row's token inside the tile
-  const int row_seen = qi < t.nq ? t.seen(qi) : 0;
-  const int least = t.seen(0), most = t.seen(t.nq - 1);
+  const int row_seen = qi < t.nq ? t.seen.of(qi) : 0;
   const uint32_t all = (1u << t.nq) - 1;
   const int* table = a.b.table + int64_t(t.b) * a.b.max_pages;
 
-  for (int pass = 0; pass < 2; ++pass) {
+  // The wave's units, every fourth of the split's. Lane i knows entry 64 win + i of the walk:
+  // the addresses of units to load need no memory access.
+  int win = -1, w_entry = 0, w_phys = -1;
+  uint32_t w_who = 0;
+  auto look = [&](int first) {
+    win = first;
+    const int i = first * 64 + lane;
+    const uint32_t x = i >= entries ? 0u : a.topk ? list[i] : all;
+    const int j = a.topk ? int(x >> 16) : i;
+    w_entry = i >= entries ? 0 : j;
+    w_phys = i >= entries ? -1 : table[j];
+    w_who = x & 0xffffu;
+  };
+  struct Unit {
+    int at;        // first key, -1: none
+    uint32_t who;  // tokens of the tile that keep its page
+  };
+  constexpr int NB = FP4 ? 4 : 2;  // units in flight
+  float* osum = (float*)(lds + (a.topk ? (a.b.max_pages * 4 + 15) / 16 * 16 : 0));
+  // only < 0: all tokens at once; else the tile's tokens one by one (see the head of the file)
+  for (int only = -1; only < t.nq; ++only) {
+    const int least = t.seen.of(max(only, 0)), most = only < 0 ? t.seen.of(t.nq - 1) : least;
+    const uint32_t ours = only < 0 ? all : 1u << only;
     w.m = kNegInf;
     w.l = 0.0f;
 #pragma unroll
     for (int c = 0; c < CT; ++c) w.o[c] = cf32x4{};
-    for (int u = u0 + wave; u < u1; u += kWaves) {
-      const int e = u / upp, kb = u - e * upp;
-      const uint32_t x = a.topk ? list[e] : uint32_t(e);
-      const int j = a.topk ? int(x >> 16) : e;
-      const uint32_t who = a.topk ? x & 0xffffu : all;
-      const int at = j * P + kb * 32;
-      if (at >= most) continue;
-      const int phys = table[j];
-      if (phys < 0 || phys >= a.c.n_pages) continue;
-      UnitLoad<D, FP4> ld;
-      load_unit<D, FP4>(a.c, (int64_t(phys) * a.c.H + t.h) * P * D, kb, lane, ld);
-      const bool full = who == all && at + 32 <= least;
-      const bool row_in = qi < t.nq && (who >> qi & 1);
-      if (pass == 0) {
-        step_unit<D, FP4>(ld, w, lane, a.scale2, at, row_seen, row_in, most, full, true);
-      } else {
-        for (int i = 0; i < t.nq; ++i)
-          step_unit<D, FP4>(ld, w, lane, a.scale2, at, row_seen, row_in,
-                            (who >> i & 1) ? t.seen(i) : 0, full, qi == i);
+    UnitLoad<D, FP4> ld[NB];
+    Unit un[NB];
+    int u = u0 + wave;
+    int64_t base = 0;
+    int kb = 0;
+    if (u < u1) look(u / upp >> 6);
+    // the next unit that holds visible tokens; past the last one its bytes are read again,
+    // so that loads need no case for the end
+    auto next = [&](Unit& x) {
+      x.at = -1;
+      while (u < u1) {
+        const int e = u / upp, k = u - e * upp;
+        if (e >> 6 != win) look(e >> 6);
+        const int phys = __builtin_amdgcn_readlane(w_phys, e & 63);
+        const int at = __builtin_amdgcn_readlane(w_entry, e & 63) * P + k * 32;
+        u += kWaves;
+        const uint32_t who = __builtin_amdgcn_readlane(w_who, e & 63) & ours;
+        if (phys < 0 || phys >= a.c.n_pages || at >= most || who == 0) continue;
+        x.at = at;
+        x.who = who;
+        base = (int64_t(phys) * a.c.H + t.h) * P * D;
+        kb = k;
+        return;
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      next(un[i]);
+      if (un[0].at < 0) break;  // nothing at all
+      load_unit<D, FP4>(a.c, base, kb, lane, ld[i]);
+    }
+    bool more = un[0].at >= 0;
+    while (more) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        if (!more) break;
+        const int at = un[i].at;
+        const uint32_t who = un[i].who;
+        const bool row_in = qi < t.nq && (who >> qi & 1);
+        if (at + 32 <= least)
+          step_unit<D, FP4, false>(ld[i], w, lane, a.scale2, at, row_seen, row_in, most);
+        else
+          step_unit<D, FP4, true>(ld[i], w, lane, a.scale2, at, row_seen, row_in, most);
+        next(un[i]);
+        load_unit<D, FP4>(a.c, base, kb, lane, ld[i]);
+        more = un[(i + 1) % NB].at >= 0;
       }
     }
-    if (pass == 0) {
+    if (only < 0 && t.nq > 1) {
       bool bad = false;
 #pragma unroll
       for (int c = 0; c < CT; ++c)
 #pragma unroll
         for (int i = 0; i < 4; ++i) bad |= !(w.o[c][i] == w.o[c][i]);
-      if (t.nq == 1 || !__any(bad)) break;
+      if (__syncthreads_or(bad)) continue;
     }
-  }
-  w.l = sum16(w.l);
+    w.l = sum16(w.l);
 
-  // the waves' results, joined in wave order
-  float* osum = (float*)lds;
-  __syncthreads();  // the list is no longer read
-  const int r = lane & 15, g = lane >> 4;
-  if (g == 0) {
-    ml[wave][r][0] = w.m;
-    ml[wave][r][1] = w.l;
-  }
-  __syncthreads();
-  float M = kNegInf;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) M = fmaxf(M, ml[i][r][0]);
-  const float f = lift(w.m, M);
-#pragma unroll
-  for (int c = 0; c < CT; ++c)
-    *(cf32x4*)(osum + (wave * 16 + r) * OROW + c * 16 + g * 4) = w.o[c] * f;
-  __syncthreads();
-  const int64_t slot = (int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * a.splits + split;
-  float* po = a.part + slot * (16 * D + 32);
-  for (int i = tid; i < 16 * (D / 4); i += kThreads) {
-    const int row = i / (D / 4), c4 = i % (D / 4);
-    const int rq = row / t.heads, gh = row - rq * t.heads;
-    if (rq >= t.nq) continue;
-    cf32x4 x{};
-    float top = kNegInf, sum = 0.0f;
-#pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
-      x += *(cf32x4*)(osum + (v * 16 + row) * OROW + c4 * 4);
-      top = fmaxf(top, ml[v][row][0]);
+    // the waves' results, joined in wave order
+    const int r = lane & 15, g = lane >> 4;
+    if (g == 0) {
+      ml[wave][r][0] = w.m;
+      ml[wave][r][1] = w.l;
     }
+    __syncthreads();
+    float M = kNegInf;
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v)
-      sum += ml[v][row][1] * lift(ml[v][row][0], top);
-    if (t.splits > 1) {
-      *(cf32x4*)(po + row * D + c4 * 4) = x;
-      if (c4 == 0) {
-        po[16 * D + row * 2] = top;
-        po[16 * D + row * 2 + 1] = sum;
+    for (int i = 0; i < kWaves; ++i) M = fmaxf(M, ml[i][r][0]);
+    const float f = lift(w.m, M);
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+      *(cf32x4*)(osum + (wave * 16 + r) * OROW + c * 16 + g * 4) = w.o[c] * f;
+    __syncthreads();
+    const int64_t slot = (int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * a.splits + split;
+    float* po = a.part + slot * (16 * D + 32);
+    for (int i = tid; i < 16 * (D / 4); i += kThreads) {
+      const int row = i / (D / 4), c4 = i % (D / 4);
+      const int rq = row / t.heads, gh = row - rq * t.heads;
+      if (rq >= t.nq || (only >= 0 && rq != only)) continue;
+      cf32x4 x{};
+      float top = kNegInf, sum = 0.0f;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) {
+        x += *(cf32x4*)(osum + (v * 16 + row) * OROW + c4 * 4);
+        top = fmaxf(top, ml[v][row][0]);
       }
-    } else {
-      const float inv = top == kNegInf ? 0.0f : 1.0f / sum;
-      const int64_t orow = int64_t(t.t0 + rq) * a.Hq + t.head0 + gh;
-      cu32x2 y;
-      y[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector(cf32x2{x[0] * inv, x[1] * inv}, cbf16x2));
-      y[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(cf32x2{x[2] * inv, x[3] * inv}, cbf16x2));
-      *(cu32x2*)(a.o + orow * D + c4 * 4) = y;
-      if (a.lse && c4 == 0) a.lse[orow] = (top + log2f(sum)) * kLn2f;
+#pragma unroll
+      for (int v = 0; v < kWaves; ++v) sum += ml[v][row][1] * lift(ml[v][row][0], top);
+      if (t.splits > 1) {
+        *(cf32x4*)(po + row * D + c4 * 4) = x;
+        if (c4 == 0) {
+          po[16 * D + row * 2] = top;
+          po[16 * D + row * 2 + 1] = sum;
+        }
+      } else {
+        write_row<D>(a, t, rq, gh, c4, x, top, sum);
+      }
     }
+    if (only < 0) break;
+    __syncthreads();
   }
 }
 
-// Joins the splits of one tile, in split order.
+// Joins the splits of one tile, in split order: a workgroup takes four rows, its threads share
+// the splits of a column piece in eight runs.
 template <int D>
 __global__ void __launch_bounds__(kThreads) cache_join_kernel(AttnArgs a) {
+  constexpr int PIECES = D / 4, RUNS = kThreads / PIECES;
+  __shared__ cf32x4 xs[RUNS][PIECES];
+  __shared__ float ws[kMaxSplits];
   Tile t;
   if (!find_tile(a, &t) || t.splits <= 1) return;
-  const int64_t slot = (int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * a.splits;
-  const float* po = a.part + slot * (16 * D + 32);
-  for (int i = threadIdx.x; i < 16 * (D / 4); i += kThreads) {
-    const int row = i / (D / 4), c4 = i % (D / 4);
-    const int rq = row / t.heads, gh = row - rq * t.heads;
-    if (rq >= t.nq) continue;
-    float top = kNegInf;
-    for (int s = 0; s < t.splits; ++s) top = fmaxf(top, po[int64_t(s) * (16 * D + 32) + 16 * D + row * 2]);
-    cf32x4 x{};
-    float sum = 0.0f;
-    for (int s = 0; s < t.splits; ++s) {
-      const float* p = po + int64_t(s) * (16 * D + 32);
-      const float m = p[16 * D + row * 2];
-      const float f = lift(m, top);
-      x += *(const cf32x4*)(p + row * D + c4 * 4) * f;
-      sum += p[16 * D + row * 2 + 1] * f;
-    }
-    const float inv = top == kNegInf ? 0.0f : 1.0f / sum;
-    const int64_t orow = int64_t(t.t0 + rq) * a.Hq + t.head0 + gh;
-    cu32x2 y;
-    y[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector(cf32x2{x[0] * inv, x[1] * inv}, cbf16x2));
-    y[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(cf32x2{x[2] * inv, x[3] * inv}, cbf16x2));
-    *(cu32x2*)(a.o + orow * D + c4 * 4) = y;
-    if (a.lse && c4 == 0) a.lse[orow] = (top + log2f(sum)) * kLn2f;
+  constexpr int64_t STRIDE = 16 * D + 32;
+  const float* po = a.part + (int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * a.splits * STRIDE;
+  const int tid = threadIdx.x, c4 = tid % PIECES, run = tid / PIECES;
+  const int row = blockIdx.z;
+  const int rq = row / t.heads, gh = row - rq * t.heads;
+  if (rq >= t.nq) return;
+  // the splits' factors, and the sum: one wave
+  __shared__ float s_top, s_sum;
+  if (tid < 64) {
+    const bool in = tid < t.splits;
+    const float m = in ? po[tid * STRIDE + 16 * D + row * 2] : kNegInf;
+    const float l = in ? po[tid * STRIDE + 16 * D + row * 2 + 1] : 0.0f;
+    float top = m;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float f = in ? lift(m, top) : 0.0f;
+    float sum = in ? l * f : 0.0f;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+    ws[tid] = f;
+    if (tid == 0) s_top = top, s_sum = sum;
   }
+  __syncthreads();
+  cf32x4 x{};
+#pragma unroll 4
+  for (int s = run; s < t.splits; s += RUNS) x += *(const cf32x4*)(po + s * STRIDE + row * D + c4 * 4) * ws[s];
+  xs[run][c4] = x;
+  __syncthreads();
+  if (run != 0) return;
+#pragma unroll
+  for (int i = 1; i < RUNS; ++i) x += xs[i][c4];
+  write_row<D>(a, t, rq, gh, c4, x, s_top, s_sum);
 }
 
 struct Plan {
+  bool chunk;
   int G, QT, RT, splits;
   int64_t items;
   int lds;
@@ -444,34 +504,37 @@ Plan plan(const DevCache& c, const DevBatch& b, int d, int Hq, int topk) {
   p.QT = p.G < 16 ? 16 / p.G : 1;
   p.RT = (p.G + 15) / 16;
   p.items = p.QT > 1 ? item_base(b.n_tokens, b.B, p.QT, 1) : b.n_tokens;
+  p.splits = 1;
+  // many rows a sequence: tiles of 128 rows share their keys, where they fill the card
+  const int64_t rows = int64_t(b.n_tokens) * p.G;
+  p.chunk = p.G <= 32 && rows >= int64_t(b.B) * 64 && rows / 128 * c.H >= 128;
+  if (p.chunk) return p;
   // workgroups without splits: tiles that hold tokens (at most), heads, row tiles
   const int64_t tiles = p.QT > 1 ? b.n_tokens / p.QT + (b.B < b.n_tokens ? b.B : b.n_tokens) : b.n_tokens;
   const int64_t wgs = tiles * c.H * p.RT;
   int64_t walk = b.max_pages;
   if (topk && int64_t(topk) * p.QT < walk) walk = int64_t(topk) * p.QT;
-  const int64_t units = walk * (c.page / 32);
-  int64_t s = (1024 + wgs - 1) / (wgs > 0 ? wgs : 1);
-  const int64_t most = (units + 4 * kWaves - 1) / (4 * kWaves);
+  int64_t s = (2 * kTargetWgs + wgs - 1) / wgs;
+  const int64_t most = (walk * (c.page / 32) + kMinUnits - 1) / kMinUnits;
   s = s < most ? s : most;
   s = s < kMaxSplits ? s : kMaxSplits;
   p.splits = int(s < 1 ? 1 : s);
-  const int merge = kWaves * 16 * (d + 4) * 4;
-  const int list = topk ? b.max_pages * 4 : 0;
-  p.lds = merge > list ? merge : list;
+  p.lds = kWaves * 16 * (d + 4) * 4 + (topk ? (b.max_pages * 4 + 15) / 16 * 16 : 0);
   return p;
 }
 
 template <int D, bool FP4>
 hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t s) {
   if (p.lds > 48 * 1024) {
-    const hipError_t e = ensure_dynamic_lds((const void*)cache_attn_kernel<D, FP4>, kCacheMaxPages * 4);
+    const hipError_t e = ensure_dynamic_lds((const void*)cache_attn_kernel<D, FP4>,
+                                            kCacheMaxPages * 4 + kWaves * 16 * (D + 4) * 4);
     if (e != hipSuccess) return e;
   }
   const unsigned ny = unsigned(a.c.H * p.RT);
   cache_attn_kernel<D, FP4><<<dim3(unsigned(p.items), ny, p.splits), kThreads, p.lds, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  cache_join_kernel<D><<<dim3(unsigned(p.items), ny), kThreads, 0, s>>>(a);
+  cache_join_kernel<D><<<dim3(unsigned(p.items), ny, 16), kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -479,7 +542,7 @@ hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t s) {
 
 size_t cache_attn_workspace_bytes(const DevCache& c, const DevBatch& b, int d, int Hq, int topk) {
   const Plan p = plan(c, b, d, Hq, topk);
-  if (p.splits == 1) return 0;
+  if (p.chunk || p.splits == 1) return 0;
   return size_t(p.items) * c.H * p.RT * p.splits * (16 * d + 32) * 4;
 }
 
@@ -503,6 +566,7 @@ hipError_t launch_cache_attn(const DevCache& c, const DevBatch& b, int d, const 
   a.lse = x.lse;
   a.part = (float*)ws;
   a.splits = p.splits;
+  if (p.chunk) return launch_chunk_attn(a, d, s);
   if (d == 128) return c.fp4 ? run<128, true>(a, p, s) : run<128, false>(a, p, s);
   return c.fp4 ? run<64, true>(a, p, s) : run<64, false>(a, p, s);
 }

@@ -1,0 +1,420 @@
+// Attention of many new queries over the paged cache (gfx950): chunks of a prompt, new
+// frames of a video.
+//
+// A workgroup takes one K/V head and a run of neighbouring tokens of one sequence: four
+// waves of 32 rows each (floor(32 / G) tokens times their G query heads). It walks the
+// union of its tokens' page lists in units of 32 keys; a unit's K and V are staged once in
+// LDS for the four waves, in the pages' fragment order, which is free of bank conflicts
+// and needs no transpose. A wave skips the pages none of its own tokens keeps. The scores
+// of a page that only some of its rows keep cost nothing to mask: a row's bias is its
+// running maximum, or infinity where the row does not keep the page.
+//
+// bf16 units go from memory to LDS directly, two units ahead of the computation in a ring
+// of three; 4-bit units are loaded two ahead into registers and widened to bf16 on the way
+// to LDS, once for four waves (V's powers of two are applied there: exact).
+//
+// S^T (32 keys x 32 rows) = K Q^T and O^T += V^T P^T with mfma 32x32x16. The lane's scores
+// are then in the order in which a V fragment holds its keys. Softmax as in cache_attn.hip;
+// the running maximum is raised only when a row's grows by more than 2^8.
+//
+// What a row must not see: see cache_attn.hip.
+#include "cache_attn.h"
+
+namespace spade {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) char lds_char;
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kRows = 32;          // rows of a wave
+constexpr int kSeg = 512;          // pages walked before the masks are built anew
+constexpr float kLazy = 8.0f;
+
+template <int D, bool FP4>
+struct Stage {
+  static constexpr int SIDE = 32 * D * 2;  // K or V of a unit in LDS
+  static constexpr int BUFS = FP4 ? 2 : 3;
+  static constexpr int LOADS = SIDE / 1024 / kWaves;  // 1 KB loads a wave and side
+  static constexpr int BYTES = BUFS * 2 * SIDE;
+};
+
+struct Seg {
+  uint32_t mask[kWaves][kSeg];  // tokens of the wave that keep the page
+  int phys[kSeg];               // kept pages in ascending order
+  uint16_t page[kSeg];          // their place in the segment
+  int wave_n[2][kWaves];
+  int n;
+};
+
+// Barrier behind which every wave has at most N loads to LDS in flight and has read what it
+// asked of LDS before (the buffers are overwritten next).
+template <int N>
+__device__ __forceinline__ void unit_barrier() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// 16 bytes a lane from base + off to LDS address dst + 16 lane.
+__device__ __forceinline__ void to_lds(const void* base, uint32_t off, uint32_t dst) {
+  asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(dst) : "memory");
+}
+
+template <typename T>
+__device__ __forceinline__ const T* uniform(const T* p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(x));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(uint32_t(x >> 32));
+  return reinterpret_cast<const T*>(uint64_t(hi) << 32 | lo);
+}
+
+// A 4-bit unit on its way: this thread's share.
+template <int D>
+struct Raw {
+  cu32x2 k, v, vs;
+  uint32_t ks;
+};
+
+template <int D>
+__device__ __forceinline__ void load_raw(const DevCache& c, int64_t base, int kb, int tid, Raw<D>& r) {
+  const uint8_t* kp = (const uint8_t*)c.k + (base >> 1) + kb * 16 * D;
+  const uint8_t* vp = (const uint8_t*)c.v + (base >> 1) + kb * 16 * D;
+  const uint8_t* ks = c.ks + (base >> 5) + kb * D;
+  const uint8_t* vs = c.vs + (base >> 5) + kb * D;
+  const int tile = tid >> 7, g = (tid >> 5) & 3, m = (tid >> 1) & 15;
+  if constexpr (D == 128) {
+    r.k = ((const cu32x2*)kp)[tid];
+    r.v = ((const cu32x2*)vp)[tid];
+    r.ks = ks[tile * 64 + g * 16 + m];
+    const int gr = (tid >> 7) * 2 + (tid & 1);  // column tiles 4 half + 2 (tid & 1) + {0, 1}
+    r.vs = ((const cu32x2*)vs)[g * 4 + gr];
+  } else {
+    r.k[0] = ((const uint32_t*)kp)[tid];
+    r.v[0] = ((const uint32_t*)vp)[tid];
+    r.ks = ks[tile * 32 + (g >> 1) * 16 + m];
+    r.vs = ((const cu32x2*)vs)[(tid >> 6) * 2 + ((tid & 3) >> 1)];
+  }
+}
+
+__device__ __forceinline__ cbf16x8 scaled_eight(uint32_t x, cu32x2 scales) {
+  float f[8];
+  const cf32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, 1.0f, 0),
+               b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, 1.0f, 1),
+               c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, 1.0f, 2),
+               d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, 1.0f, 3);
+  f[0] = a[0], f[1] = a[1], f[2] = b[0], f[3] = b[1], f[4] = c[0], f[5] = c[1], f[6] = d[0], f[7] = d[1];
+  cbf16x8 y;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    y[i] = (__bf16)(f[i] * scale_of((scales[i >> 2] >> (8 * (i & 3))) & 255u));
+  return y;
+}
+
+template <int D>
+__device__ __forceinline__ void store_raw(const Raw<D>& r, char* buf, int tid) {
+  const int tile = tid >> 7, g = (tid >> 5) & 3, m = (tid >> 1) & 15;
+  constexpr int W = D / 64;  // dwords a thread and side
+  const float s = scale_of(r.ks);
+#pragma unroll
+  for (int i = 0; i < W; ++i) {
+    const int ch = g * (D / 4) + ((tid & 1) * W + i) * 8;  // first of 8 channels
+    *(cbf16x8*)(buf + ((tile * (D / 32) + (ch >> 5)) * 64 + ((ch & 31) >> 3) * 16 + m) * 16) =
+        fp4_eight(r.k[i], s);
+  }
+  char* vb = buf + Stage<D, true>::SIDE;
+  if constexpr (D == 128) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int ct = (tid >> 7) * 4 + (tid & 1) * 2 + i;
+      *(cbf16x8*)(vb + ((ct * 4 + g) * 16 + m) * 16) = scaled_eight(r.v[i], r.vs);
+    }
+  } else {
+    const int ct = tid & 3;
+    *(cbf16x8*)(vb + ((ct * 4 + (tid >> 6)) * 16 + ((tid >> 2) & 15)) * 16) = scaled_eight(r.v[0], r.vs);
+  }
+}
+
+__device__ __forceinline__ float row_max(float v) {  // over the two lanes of a row
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+
+template <int D>
+struct Rows {
+  cbf16x8 q[D / 16];
+  f32x16 o[D / 32];
+  float m, l;
+};
+
+// One staged unit, keys at..at+31. row_in: the lane's row keeps the page. EDGE: a row sees the
+// keys below row_seen, and V is cleared from key v_seen on.
+template <int D, bool EDGE>
+__device__ __forceinline__ void step(const char* kf, const char* vf, Rows<D>& w, int lane, float scale2,
+                                     int at, int row_seen, bool row_in, int v_seen) {
+  const int half = lane >> 5;
+  f32x16 s = {};
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k)
+    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+        *(const cbf16x8*)(kf + (k >> 1) * 1024 + (k & 1) * 512), w.q[k], s, 0, 0, 0);
+  if constexpr (EDGE) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      s[i] = at + 8 * (i >> 2) + 4 * half + (i & 3) < row_seen ? s[i] : kNegInf;
+  }
+  float top = fmaxf(s[0], s[1]);
+#pragma unroll
+  for (int i = 2; i < 16; i += 2) top = fmaxf(fmaxf(top, s[i]), s[i + 1]);
+  top = row_max(top) * scale2;
+  top = row_in ? top : kNegInf;
+  float m = w.m;
+  if (__any(top > m + kLazy)) {
+    m = top > m + kLazy ? top : m;
+    const float alpha = w.m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(w.m - m);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) w.o[c] *= alpha;
+    w.l *= alpha;
+    w.m = m;
+  }
+  const float bias = row_in && m != kNegInf ? -m : kNegInf;
+  float sum = 0.0f;
+  cbf16x8 p[2];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], scale2, bias));
+    sum += e;
+    // key 8 (i / 4) + 4 half + i % 4: V fragment 2 t + half holds i / 4 = t and t + 2
+    p[(i >> 2) & 1][(i >> 3) * 4 + (i & 3)] = (__bf16)e;
+  }
+  w.l += sum;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      cbf16x8 f = *(const cbf16x8*)(vf + c * 2048 + t * 512);
+      if constexpr (EDGE) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int key = at + (i >> 2) * 16 + (2 * t + half) * 4 + (i & 3);
+          f[i] = key < v_seen ? f[i] : (__bf16)0.0f;
+        }
+      }
+      w.o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p[t], w.o[c], 0, 0, 0);
+    }
+}
+
+template <int D, bool FP4>
+__global__ void __launch_bounds__(kThreads, 2) cache_chunk_kernel(AttnArgs a, int64_t items) {
+  using ST = Stage<D, FP4>;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  __shared__ Seg sg;
+  // each XCD takes a run of neighbouring items of a head: they want the same pages
+  const int64_t total = items * a.c.H, per = (total + 7) >> 3;
+  const int64_t slot = blockIdx.x >> 3, L = (blockIdx.x & 7) * per + slot;
+  if (slot >= per || L >= total) return;
+  const int h = int(L / items);
+  const SeqItem it = find_item(a.b, L - h * items, a.QT, 1, kThreads);
+  if (it.b < 0) return;
+  const int skip = it.first * a.QT;
+  if (skip >= it.n) return;
+  const int t0 = it.t0 + skip, nq = min(a.QT, it.n - skip);
+  Seen seen = seen_of(a, it.b, it.n);
+  seen.first += skip * seen.step;
+  const int P = a.c.page, upp = P >> 5;
+  const int pages = (seen.of(nq - 1) + P - 1) / P;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  // the wave's tokens q0..q0+qn-1 of the tile, the lane's row
+  const int QW = a.QT / kWaves, q0 = wave * QW, qn = min(max(nq - q0, 0), QW);
+  const int r = lane & 31, half = lane >> 5;
+  const int qi = r / a.G, gh = r - qi * a.G;
+  const bool live = qi < qn;
+  const int row_seen = live ? seen.of(q0 + qi) : 0;
+  const uint32_t all = qn ? 0xffffffffu >> (32 - qn) : 0;
+  const int64_t orow = int64_t(t0 + q0 + qi) * a.Hq + h * a.G + gh;
+
+  Rows<D> w;
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k)
+    w.q[k] = live ? *(const cbf16x8*)(a.q + orow * D + (k >> 1) * 32 + ((k & 1) * 2 + half) * 8)
+                  : cbf16x8{};
+  const int* table = a.b.table + int64_t(it.b) * a.b.max_pages;
+  const int kf_lane = ((lane >> 4) & 1) * (D * 32) + half * 256 + (lane & 15) * 16;
+  const int vf_lane = ((lane >> 4) & 1) * 1024 + half * 256 + (lane & 15) * 16;
+  const uint32_t lds0 = uint32_t(uintptr_t((lds_char*)lds));
+
+  // only < 0: all tokens at once; else every wave's tokens one by one (see cache_attn.hip)
+  for (int only = -1; only < QW; ++only) {
+    const int least = qn ? seen.of(q0 + max(only, 0)) : 0;
+    const int most = only < 0 ? (qn ? seen.of(q0 + qn - 1) : 0) : only < qn ? least : 0;
+    const uint32_t ours = only < 0 ? all : 1u << only;
+    w.m = kNegInf;
+    w.l = 0.0f;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) w.o[c] = f32x16{};
+    for (int seg0 = 0; seg0 < pages; seg0 += kSeg) {
+      const int span = min(kSeg, pages - seg0);
+      __syncthreads();  // the last segment's masks are no longer read
+      if (a.topk) {
+        for (int i = tid; i < kSeg; i += kThreads)
+#pragma unroll
+          for (int v = 0; v < kWaves; ++v) sg.mask[v][i] = 0;
+        __syncthreads();
+        const int64_t row0 = int64_t(t0) * a.c.H + h;
+        for (int i = tid; i < nq * a.topk; i += kThreads) {
+          const int q = i / a.topk, k = i - q * a.topk;
+          const int64_t row = row0 + int64_t(q) * a.c.H;
+          if (k >= a.counts[row]) continue;
+          const int j = a.indices[row * a.topk + k];
+          if (j >= seg0 && j < seg0 + span && j * P < seen.of(q))
+            atomicOr(&sg.mask[q / QW][j - seg0], 1u << (q % QW));
+        }
+        __syncthreads();
+      }
+      // the pages that count, in order
+      int base_n = 0;
+#pragma unroll
+      for (int round = 0; round < kSeg / kThreads; ++round) {
+        const int i = round * kThreads + tid;
+        int phys = -1;
+        if (i < span && (!a.topk || (sg.mask[0][i] | sg.mask[1][i] | sg.mask[2][i] | sg.mask[3][i])))
+          phys = table[seg0 + i];
+        const bool ok = phys >= 0 && phys < a.c.n_pages;
+        const uint64_t bits = __ballot(ok);
+        if (lane == 0) sg.wave_n[round][wave] = __popcll(bits);
+        __syncthreads();
+        int at = base_n + __popcll(bits & ((uint64_t(1) << lane) - 1));
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) {
+          at += v < wave ? sg.wave_n[round][v] : 0;
+          base_n += sg.wave_n[round][v];
+        }
+        if (ok) {
+          sg.phys[at] = phys;
+          sg.page[at] = uint16_t(i);
+        }
+      }
+      __syncthreads();
+      const int units = base_n * upp;
+
+      // the cursor of the loads: two units ahead of the computation
+      int le = 0, lkb = 0;
+      auto page_base = [&](int e) {
+        return (int64_t(__builtin_amdgcn_readfirstlane(sg.phys[e])) * a.c.H + h) * P * D;
+      };
+      auto advance = [&] {
+        if (++lkb == upp) lkb = 0, ++le;
+      };
+      auto fetch = [&](int buf) {  // bf16
+        const int64_t base = page_base(le) + lkb * (32 * D);
+        const char* kp = (const char*)uniform((const __bf16*)a.c.k + base);
+        const char* vp = (const char*)uniform((const __bf16*)a.c.v + base);
+        const uint32_t dst = lds0 + buf * 2 * ST::SIDE;
+#pragma unroll
+        for (int i = 0; i < ST::LOADS; ++i) {
+          const uint32_t off = (wave * ST::LOADS + i) * 1024;
+          to_lds(kp, off + lane * 16, dst + off);
+          to_lds(vp, off + lane * 16, dst + ST::SIDE + off);
+        }
+        advance();
+      };
+      Raw<D> raw;
+      auto fetch_raw = [&] {
+        load_raw<D>(a.c, page_base(le), lkb, tid, raw);
+        advance();
+      };
+      if constexpr (FP4) {
+        if (units > 0) {
+          fetch_raw();
+          store_raw<D>(raw, lds, tid);
+          if (units > 1) fetch_raw();
+        }
+      } else {
+        if (units > 0) fetch(0);
+        if (units > 1) fetch(1);
+      }
+      int e = 0, kb = 0, buf = 0;
+      for (int u = 0; u < units; ++u) {
+        if constexpr (FP4) {
+          lds_barrier();
+          if (u + 1 < units) store_raw<D>(raw, lds + (buf ^ 1) * 2 * ST::SIDE, tid);
+          if (u + 2 < units) fetch_raw();
+        } else {
+          if (u + 1 < units) unit_barrier<2 * ST::LOADS>();
+          else unit_barrier<0>();
+          if (u + 2 < units) fetch(buf == 0 ? 2 : buf - 1);
+        }
+        const int page = sg.page[e];
+        const uint32_t who = (a.topk ? __builtin_amdgcn_readfirstlane(sg.mask[wave][page]) : all) & ours;
+        const int at = (seg0 + __builtin_amdgcn_readfirstlane(page)) * P + kb * 32;
+        if (who && at < most) {
+          const char* kf = lds + buf * 2 * ST::SIDE + kf_lane;
+          const char* vf = lds + buf * 2 * ST::SIDE + ST::SIDE + vf_lane;
+          const bool row_in = live && (who >> qi & 1);
+          if (at + 32 <= least) step<D, false>(kf, vf, w, lane, a.scale2, at, row_seen, row_in, most);
+          else step<D, true>(kf, vf, w, lane, a.scale2, at, row_seen, row_in, most);
+        }
+        if (++kb == upp) kb = 0, ++e;
+        buf = buf + 1 == ST::BUFS ? 0 : buf + 1;
+      }
+    }
+    if (only < 0 && QW > 1) {
+      bool bad = false;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) bad |= !(w.o[c][i] == w.o[c][i]);
+      if (__syncthreads_or(bad)) continue;
+    }
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(w.l), __float_as_uint(w.l), false, false);
+    const float l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    if (live && (only < 0 || qi == only)) {
+      const float inv = w.m == kNegInf ? 0.0f : 1.0f / l;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const cf32x2 x = {w.o[c][i] * inv, w.o[c][i + 1] * inv}, y = {w.o[c][i + 2] * inv, w.o[c][i + 3] * inv};
+          *(cu32x2*)(a.o + orow * D + c * 32 + 2 * i + 4 * half) =
+              cu32x2{__builtin_bit_cast(uint32_t, __builtin_convertvector(x, cbf16x2)),
+                     __builtin_bit_cast(uint32_t, __builtin_convertvector(y, cbf16x2))};
+        }
+      if (a.lse && half == 0) a.lse[orow] = (w.m + log2f(l)) * kLn2f;
+    }
+    if (only < 0) break;
+  }
+}
+
+template <int D, bool FP4>
+hipError_t run(const AttnArgs& a, int64_t items, hipStream_t s) {
+  const int bytes = Stage<D, FP4>::BYTES;
+  if (bytes > 32 * 1024) {
+    const hipError_t e = ensure_dynamic_lds((const void*)cache_chunk_kernel<D, FP4>, bytes);
+    if (e != hipSuccess) return e;
+  }
+  const int64_t wgs = (items * a.c.H + 7) / 8 * 8;
+  cache_chunk_kernel<D, FP4><<<dim3(unsigned(wgs)), kThreads, bytes, s>>>(a, items);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t chunk_items(const DevCache& c, const DevBatch& b, int Hq) {
+  const int G = Hq / c.H;
+  if (G > kRows) return 0;
+  return item_base(b.n_tokens, b.B, kRows / G * kWaves, 1);
+}
+
+hipError_t launch_chunk_attn(const AttnArgs& x, int d, hipStream_t s) {
+  AttnArgs a = x;
+  a.QT = kRows / a.G * kWaves;
+  const int64_t items = chunk_items(a.c, a.b, a.Hq);
+  if (d == 128) return a.c.fp4 ? run<128, true>(a, items, s) : run<128, false>(a, items, s);
+  return a.c.fp4 ? run<64, true>(a, items, s) : run<64, false>(a, items, s);
+}
+
+}  // namespace spade
