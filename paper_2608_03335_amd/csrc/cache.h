@@ -132,6 +132,24 @@ __device__ __forceinline__ SeqItem find_item(const DevBatch& bt, int64_t item, i
 // infinity, and the group's values are stored as 0: 0 * inf is NaN wherever it is used.
 __device__ __forceinline__ float scale_of(uint32_t code) { return __uint_as_float(code << 23); }
 
+// The scales of a dword's four codes, one instruction each.
+__device__ __forceinline__ void scales_of(uint32_t w, float* s) {
+  uint32_t r;
+  const uint32_t n = 23;
+  asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0"
+      : "=v"(r) : "v"(n), "v"(w));
+  s[0] = __uint_as_float(r);
+  asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1"
+      : "=v"(r) : "v"(n), "v"(w));
+  s[1] = __uint_as_float(r);
+  asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2"
+      : "=v"(r) : "v"(n), "v"(w));
+  s[2] = __uint_as_float(r);
+  asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3"
+      : "=v"(r) : "v"(n), "v"(w));
+  s[3] = __uint_as_float(r);
+}
+
 // bf16 pair from byte BYTE of x, times scale (a power of two: exact)
 template <int BYTE>
 __device__ __forceinline__ cbf16x2 fp4_pair(uint32_t x, float scale) {

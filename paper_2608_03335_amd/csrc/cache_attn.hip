@@ -170,14 +170,15 @@ __device__ __forceinline__ void load_q(const AttnArgs& a, const Tile& t, int lan
   }
 }
 
-// One unit: keys at..at+31 of the sequence. row_in: the lane's row keeps the page. EDGE: a row
-// sees the keys below row_seen, and V is cleared from key v_seen on.
-template <int D, bool FP4, bool EDGE>
-__device__ __forceinline__ void step_unit(const UnitLoad<D, FP4>& u, Wave<D, FP4>& w, int lane,
-                                          float scale2, int at, int row_seen, bool row_in,
-                                          int v_seen) {
+// One unit: keys at..at+31 of the sequence. row_in: the lane's row keeps the page. edge (the
+// same for all lanes): a row sees the keys below row_seen, and V is cleared from key v_seen on.
+template <int D, bool FP4>
+__device__ __forceinline__ void step_unit(UnitLoad<D, FP4>& u, Wave<D, FP4>& w, int lane,
+                                          float scale2, int at, bool edge, int row_seen,
+                                          bool row_in, int v_seen) {
   constexpr int KK = D / 32, CT = D / 16;
   const int g = lane >> 4;
+  const int key0 = at + g * 4;  // the lane's keys: key0 + {0..3, 16..19}
   cf32x4 s[2] = {};
 #pragma unroll
   for (int k = 0; k < KK; ++k)
@@ -190,10 +191,10 @@ __device__ __forceinline__ void step_unit(const UnitLoad<D, FP4>& u, Wave<D, FP4
     }
   float p[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    p[i] = s[i >> 2][i & 3];
-    if constexpr (EDGE) p[i] = at + (i >> 2) * 16 + g * 4 + (i & 3) < row_seen ? p[i] : kNegInf;
-  }
+  for (int i = 0; i < 8; ++i) p[i] = s[i >> 2][i & 3];
+  if (edge)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = key0 + (i >> 2) * 16 + (i & 3) < row_seen ? p[i] : kNegInf;
   float top = fmaxf(p[0], p[1]);
 #pragma unroll
   for (int i = 2; i < 8; i += 2) top = fmaxf(fmaxf(top, p[i]), p[i + 1]);
@@ -217,39 +218,97 @@ __device__ __forceinline__ void step_unit(const UnitLoad<D, FP4>& u, Wave<D, FP4
     sum += p[i];
   }
   w.l += sum;
-  auto add = [&](int c, cbf16x8 f, cbf16x8 pf) {
-    w.o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, pf, w.o[c], 0, 0, 0);
-  };
   if constexpr (!FP4) {
+    if (edge) {
+      uint32_t keep[4];  // halves of a V fragment's dwords
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = key0 + (i >> 1) * 16 + (i & 1) * 2;
+        keep[i] = (key < v_seen ? 0xffffu : 0u) | (key + 1 < v_seen ? 0xffff0000u : 0u);
+      }
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u.v[c][i] &= keep[i];
+    }
     cbf16x8 pf;
 #pragma unroll
     for (int i = 0; i < 8; ++i) pf[i] = (__bf16)p[i];
 #pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      cbf16x8 f = __builtin_bit_cast(cbf16x8, u.v[c]);
-      if constexpr (EDGE)
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          f[i] = at + (i >> 2) * 16 + g * 4 + (i & 3) < v_seen ? f[i] : (__bf16)0.0f;
-      add(c, f, pf);
-    }
+    for (int c = 0; c < CT; ++c)
+      w.o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(cbf16x8, u.v[c]), pf, w.o[c], 0, 0, 0);
   } else {
+    if (edge) {  // scale 2^-127 becomes 0 for a key nobody sees: p is 0, its V code is finite
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        uint32_t keep = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) keep |= key0 + i * 16 + j < v_seen ? 255u << (8 * j) : 0u;
+#pragma unroll
+        for (int gr = 0; gr < D / 32; ++gr) u.vs[gr][i] &= keep;
+      }
+    }
 #pragma unroll
     for (int gr = 0; gr < D / 32; ++gr) {
+      float two[8];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) scales_of(u.vs[gr][i], two + 4 * i);
       cbf16x8 pf;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float two = scale_of((u.vs[gr][i >> 2] >> (8 * (i & 3))) & 255u);
-        if constexpr (EDGE) two = at + (i >> 2) * 16 + g * 4 + (i & 3) < v_seen ? two : 0.0f;
-        pf[i] = (__bf16)(p[i] * two);
-      }
+      for (int i = 0; i < 8; ++i) pf[i] = (__bf16)(p[i] * two[i]);
 #pragma unroll
       for (int cc = 0; cc < 2; ++cc) {
         const int c = gr * 2 + cc;
-        add(c, fp4_eight(u.v[c >> 2][c & 3], 1.0f), pf);
+        w.o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp4_eight(u.v[c >> 2][c & 3], 1.0f), pf, w.o[c], 0, 0, 0);
       }
     }
   }
+}
+
+// The pages the tile walks, ascending, in LDS; their number.
+__device__ __forceinline__ int build_list(const AttnArgs& a, const Tile& t, uint32_t* list) {
+  __shared__ int s_len;
+  const int tid = threadIdx.x, lane = tid & 63, P = a.c.page;
+  const int64_t row0 = int64_t(t.t0) * a.c.H + t.h;
+  if (t.nq == 1) {  // one token's list, as selections write it, is the walk already
+    const int n = min(max(a.counts[row0], 0), a.topk);
+    bool good = true;
+    for (int k = tid; k < n; k += kThreads) {
+      const int j = a.indices[row0 * a.topk + k];
+      const int before = k ? a.indices[row0 * a.topk + k - 1] : -1;
+      good &= j > before && j < t.pages;
+      list[k] = uint32_t(j) << 16 | 1u;
+    }
+    // as many entries as the table has pages fit: a longer list cannot ascend
+    if (n <= a.b.max_pages && __syncthreads_and(good)) return n;
+    __syncthreads();
+  }
+  for (int j = tid; j < t.pages; j += kThreads) list[j] = 0;
+  __syncthreads();
+  for (int i = 0; i < t.nq; ++i) {
+    const int64_t row = row0 + int64_t(i) * a.c.H;
+    const int n = min(max(a.counts[row], 0), a.topk);
+    const int vis = (t.seen.of(i) + P - 1) / P;
+    for (int k = tid; k < n; k += kThreads) {
+      const int j = a.indices[row * a.topk + k];
+      if (j >= 0 && j < vis) atomicOr(&list[j], 1u << i);
+    }
+  }
+  __syncthreads();
+  if (tid < 64) {  // compaction in place: entry e comes from a page >= e
+    int n = 0;
+    for (int j0 = 0; j0 < t.pages; j0 += 64) {
+      const int j = j0 + lane;
+      const uint32_t x = j < t.pages ? list[j] : 0;
+      const uint64_t bits = __ballot(x != 0);
+      const int at = n + __popcll(bits & ((uint64_t(1) << lane) - 1));
+      if (x) list[at] = uint32_t(j) << 16 | x;
+      n += __popcll(bits);
+    }
+    if (lane == 0) s_len = n;
+  }
+  __syncthreads();
+  return s_len;
 }
 
 // Four channels of a finished row.
@@ -266,76 +325,49 @@ __device__ __forceinline__ void write_row(const AttnArgs& a, const Tile& t, int 
 }
 
 template <int D, bool FP4>
-__global__ void __launch_bounds__(kThreads, 2) cache_attn_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kThreads, FP4 ? 3 : 2) cache_attn_kernel(AttnArgs a) {
   constexpr int CT = D / 16;
   constexpr int OROW = D + 4;  // fp32 row of the waves' merge in LDS
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float ml[kWaves][16][2];
-  __shared__ int s_len;
   Tile t;
   if (!find_tile(a, &t)) return;
   const int split = blockIdx.z;
   if (split >= t.splits) return;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int P = a.c.page, upp = P >> 5;
+  Wave<D, FP4> w;
+  load_q(a, t, lane, w);
   uint32_t* list = (uint32_t*)lds;  // entries: page << 16 | tokens of the tile that keep it
   int entries = t.pages;
-  if (a.topk) {
-    for (int j = tid; j < t.pages; j += kThreads) list[j] = 0;
-    __syncthreads();
-    for (int i = 0; i < t.nq; ++i) {
-      const int64_t row = int64_t(t.t0 + i) * a.c.H + t.h;
-      const int n = min(max(a.counts[row], 0), a.topk);
-      const int vis = (t.seen.of(i) + P - 1) / P;
-      for (int k = tid; k < n; k += kThreads) {
-        const int j = a.indices[row * a.topk + k];
-        if (j >= 0 && j < vis) atomicOr(&list[j], 1u << i);
-      }
-    }
-    __syncthreads();
-    if (wave == 0) {  // compaction in place: entry e comes from a page >= e
-      int n = 0;
-      for (int j0 = 0; j0 < t.pages; j0 += 64) {
-        const int j = j0 + lane;
-        const uint32_t x = j < t.pages ? list[j] : 0;
-        const uint64_t bits = __ballot(x != 0);
-        const int at = n + __popcll(bits & ((uint64_t(1) << lane) - 1));
-        if (x) list[at] = uint32_t(j) << 16 | x;
-        n += __popcll(bits);
-      }
-      if (lane == 0) s_len = n;
-    }
-    __syncthreads();
-    entries = s_len;
-  }
+  if (a.topk) entries = build_list(a, t, list);
   const int units = entries * upp;
   const int u0 = int(int64_t(units) * split / t.splits), u1 = int(int64_t(units) * (split + 1) / t.splits);
 
-  Wave<D, FP4> w;
-  load_q(a, t, lane, w);
   const int qi = (lane & 15) / t.heads;  // the row's token inside the tile
   const int row_seen = qi < t.nq ? t.seen.of(qi) : 0;
   const uint32_t all = (1u << t.nq) - 1;
   const int* table = a.b.table + int64_t(t.b) * a.b.max_pages;
 
-  // The wave's units, every fourth of the split's. Lane i knows entry 64 win + i of the walk:
-  // the addresses of units to load need no memory access.
+  // The wave's units, every fourth of the split's. Lane i knows entry 64 win + i of the walk,
+  // so the address of a unit to load needs no memory access but every 64 pages.
   int win = -1, w_entry = 0, w_phys = -1;
   uint32_t w_who = 0;
   auto look = [&](int first) {
     win = first;
     const int i = first * 64 + lane;
     const uint32_t x = i >= entries ? 0u : a.topk ? list[i] : all;
-    const int j = a.topk ? int(x >> 16) : i;
-    w_entry = i >= entries ? 0 : j;
-    w_phys = i >= entries ? -1 : table[j];
+    w_entry = i >= entries ? 0 : a.topk ? int(x >> 16) : i;
+    w_phys = i >= entries ? -1 : table[w_entry];
     w_who = x & 0xffffu;
+    asm volatile("" : "+v"(w_phys));  // waited for here, not at every use
   };
   struct Unit {
-    int at;        // first key, -1: none
-    uint32_t who;  // tokens of the tile that keep its page
+    int at;        // first key
+    uint32_t who;  // tokens of the tile that keep its page; 0: nothing to compute
   };
-  constexpr int NB = FP4 ? 4 : 2;  // units in flight
+  constexpr int NB = 2;  // units in flight
   float* osum = (float*)(lds + (a.topk ? (a.b.max_pages * 4 + 15) / 16 * 16 : 0));
   // only < 0: all tokens at once; else the tile's tokens one by one (see the head of the file)
   for (int only = -1; only < t.nq; ++only) {
@@ -348,49 +380,31 @@ __global__ void __launch_bounds__(kThreads, 2) cache_attn_kernel(AttnArgs a) {
     UnitLoad<D, FP4> ld[NB];
     Unit un[NB];
     int u = u0 + wave;
-    int64_t base = 0;
-    int kb = 0;
-    if (u < u1) look(u / upp >> 6);
-    // the next unit that holds visible tokens; past the last one its bytes are read again,
-    // so that loads need no case for the end
-    auto next = [&](Unit& x) {
-      x.at = -1;
-      while (u < u1) {
-        const int e = u / upp, k = u - e * upp;
-        if (e >> 6 != win) look(e >> 6);
-        const int phys = __builtin_amdgcn_readlane(w_phys, e & 63);
-        const int at = __builtin_amdgcn_readlane(w_entry, e & 63) * P + k * 32;
-        u += kWaves;
-        const uint32_t who = __builtin_amdgcn_readlane(w_who, e & 63) & ours;
-        if (phys < 0 || phys >= a.c.n_pages || at >= most || who == 0) continue;
-        x.at = at;
-        x.who = who;
-        base = (int64_t(phys) * a.c.H + t.h) * P * D;
-        kb = k;
-        return;
-      }
+    // A unit that holds nothing for the tile (a page outside the pool, past the walk's end)
+    // still loads, from page 0: the loads in flight are then the same on every path, and no
+    // wait has to assume the worst.
+    auto next = [&](Unit& x, UnitLoad<D, FP4>& to) {
+      const int e = u / upp, kb = u - e * upp;
+      if (u < u1 && e >> 6 != win) look(e >> 6);
+      const int phys = __builtin_amdgcn_readlane(w_phys, e & 63);
+      const bool ok = u < u1 && phys >= 0 && phys < a.c.n_pages;
+      x.at = __builtin_amdgcn_readlane(w_entry, e & 63) * P + kb * 32;
+      x.who = ok && x.at < most ? __builtin_amdgcn_readlane(w_who, e & 63) & ours : 0u;
+      load_unit<D, FP4>(a.c, (int64_t(x.who ? phys : 0) * a.c.H + t.h) * P * D, kb, lane, to);
+      u += kWaves;
     };
 #pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      next(un[i]);
-      if (un[0].at < 0) break;  // nothing at all
-      load_unit<D, FP4>(a.c, base, kb, lane, ld[i]);
-    }
-    bool more = un[0].at >= 0;
-    while (more) {
+    for (int i = 0; i < NB; ++i) next(un[i], ld[i]);
+    int mine = (u1 - u0 - wave + kWaves - 1) / kWaves;
+    while (mine > 0) {
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
-        if (!more) break;
-        const int at = un[i].at;
         const uint32_t who = un[i].who;
         const bool row_in = qi < t.nq && (who >> qi & 1);
-        if (at + 32 <= least)
-          step_unit<D, FP4, false>(ld[i], w, lane, a.scale2, at, row_seen, row_in, most);
-        else
-          step_unit<D, FP4, true>(ld[i], w, lane, a.scale2, at, row_seen, row_in, most);
-        next(un[i]);
-        load_unit<D, FP4>(a.c, base, kb, lane, ld[i]);
-        more = un[(i + 1) % NB].at >= 0;
+        step_unit<D, FP4>(ld[i], w, lane, a.scale2, un[i].at, who == 0 || un[i].at + 32 > least,
+                          who ? row_seen : 0, row_in, who ? most : 0);
+        if (--mine <= 0) break;
+        next(un[i], ld[i]);
       }
     }
     if (only < 0 && t.nq > 1) {
@@ -448,47 +462,42 @@ __global__ void __launch_bounds__(kThreads, 2) cache_attn_kernel(AttnArgs a) {
   }
 }
 
-// Joins the splits of one tile, in split order: a workgroup takes four rows, its threads share
-// the splits of a column piece in eight runs.
+// Joins the splits of one tile, in split order: a wave takes one row.
 template <int D>
 __global__ void __launch_bounds__(kThreads) cache_join_kernel(AttnArgs a) {
-  constexpr int PIECES = D / 4, RUNS = kThreads / PIECES;
-  __shared__ cf32x4 xs[RUNS][PIECES];
-  __shared__ float ws[kMaxSplits];
+  constexpr int PIECES = D / 4, RUNS = 64 / PIECES;
+  constexpr int64_t STRIDE = 16 * D + 32;
   Tile t;
   if (!find_tile(a, &t) || t.splits <= 1) return;
-  constexpr int64_t STRIDE = 16 * D + 32;
-  const float* po = a.part + (int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * a.splits * STRIDE;
-  const int tid = threadIdx.x, c4 = tid % PIECES, run = tid / PIECES;
-  const int row = blockIdx.z;
+  const int lane = threadIdx.x & 63, c4 = lane % PIECES, run = lane / PIECES;
+  const int row = blockIdx.z * kWaves + (threadIdx.x >> 6);
   const int rq = row / t.heads, gh = row - rq * t.heads;
   if (rq >= t.nq) return;
-  // the splits' factors, and the sum: one wave
-  __shared__ float s_top, s_sum;
-  if (tid < 64) {
-    const bool in = tid < t.splits;
-    const float m = in ? po[tid * STRIDE + 16 * D + row * 2] : kNegInf;
-    const float l = in ? po[tid * STRIDE + 16 * D + row * 2 + 1] : 0.0f;
-    float top = m;
+  const float* po = a.part + (int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * a.splits * STRIDE;
+  static_assert(kMaxSplits <= 64, "a lane holds one split's statistics");
+  const bool in = lane < t.splits;
+  const float m = in ? po[lane * STRIDE + 16 * D + row * 2] : kNegInf;
+  const float l = in ? po[lane * STRIDE + 16 * D + row * 2 + 1] : 0.0f;
+  float top = m;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    const float f = in ? lift(m, top) : 0.0f;
-    float sum = in ? l * f : 0.0f;
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  const float f = in ? lift(m, top) : 0.0f;
+  float sum = in ? l * f : 0.0f;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-    ws[tid] = f;
-    if (tid == 0) s_top = top, s_sum = sum;
-  }
-  __syncthreads();
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
   cf32x4 x{};
 #pragma unroll 4
-  for (int s = run; s < t.splits; s += RUNS) x += *(const cf32x4*)(po + s * STRIDE + row * D + c4 * 4) * ws[s];
-  xs[run][c4] = x;
-  __syncthreads();
-  if (run != 0) return;
+  for (int s0 = 0; s0 < t.splits; s0 += RUNS) {
+    const int s = min(s0 + run, t.splits - 1);
+    const float fs = __shfl(f, s);
+    const cf32x4 y = *(const cf32x4*)(po + s * STRIDE + row * D + c4 * 4);
+    if (s0 + run < t.splits) x += y * fs;
+  }
 #pragma unroll
-  for (int i = 1; i < RUNS; ++i) x += xs[i][c4];
-  write_row<D>(a, t, rq, gh, c4, x, s_top, s_sum);
+  for (int o = PIECES; o < 64; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] += __shfl_xor(x[i], o);
+  if (run == 0) write_row<D>(a, t, rq, gh, c4, x, top, sum);
 }
 
 struct Plan {
@@ -513,7 +522,8 @@ Plan plan(const DevCache& c, const DevBatch& b, int d, int Hq, int topk) {
   const int64_t tiles = p.QT > 1 ? b.n_tokens / p.QT + (b.B < b.n_tokens ? b.B : b.n_tokens) : b.n_tokens;
   const int64_t wgs = tiles * c.H * p.RT;
   int64_t walk = b.max_pages;
-  if (topk && int64_t(topk) * p.QT < walk) walk = int64_t(topk) * p.QT;
+  const int64_t each = (int64_t(b.n_tokens) + b.B - 1) / b.B;  // tokens a sequence, on average
+  if (topk && topk * (each < p.QT ? each : p.QT) < walk) walk = topk * (each < p.QT ? each : p.QT);
   int64_t s = (2 * kTargetWgs + wgs - 1) / wgs;
   const int64_t most = (walk * (c.page / 32) + kMinUnits - 1) / kMinUnits;
   s = s < most ? s : most;
@@ -534,7 +544,8 @@ hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t s) {
   cache_attn_kernel<D, FP4><<<dim3(unsigned(p.items), ny, p.splits), kThreads, p.lds, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  cache_join_kernel<D><<<dim3(unsigned(p.items), ny, 16), kThreads, 0, s>>>(a);
+  const int rows = p.QT * (p.G < 16 ? p.G : 16);
+  cache_join_kernel<D><<<dim3(unsigned(p.items), ny, (rows + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
