@@ -92,40 +92,70 @@ typedef uint32_t cu32x2 __attribute__((ext_vector_type(2)));
 // floor(cu[b+1] / unit) - floor(cu[b] / unit) + extra items, a sum that telescopes, so
 // item ranges need no scan over the sequences and the host knows their total.
 struct SeqItem {
-  int b;      // -1: no such item
-  int first;  // index of the item inside the sequence
-  int t0, n;  // the sequence's new tokens
+  int b;         // -1: no such item
+  int first;     // index of the item inside the sequence
+  int t0, n;     // the sequence's new tokens (inside from..to)
+  int start, all;  // its first new token and their number, whatever from and to
+  int64_t len;   // tokens in its cache, as given
 };
 
-__host__ __device__ inline int64_t item_base(int tokens, int b, int unit, int extra) {
-  return int64_t(tokens) / unit + int64_t(extra) * b;
+// (at most 2^28 tokens and 2^20 sequences: 32 bits hold it)
+__host__ __device__ inline int item_base(int tokens, int b, int unit, int extra) {
+  return tokens / unit + extra * b;
 }
 
-// Finds the sequence of a work item: every thread of the block tests some sequences, so
-// the search costs one load, not log2(B) of them. All threads of the block must call.
-// Offsets that do not ascend cannot lead out of the batch's arrays: an item then belongs
-// to one of the sequences that claim it, or to none.
-__device__ __forceinline__ SeqItem find_item(const DevBatch& bt, int64_t item, int unit, int extra,
-                                             int threads) {
-  __shared__ int hit;
+// Finds the sequence of a work item among the tokens from..to-1: every thread of the block
+// looks at some sequences, so the search and the sequence's length cost one load latency
+//. All threads of
+// the block must call. Offsets that do not ascend cannot lead out of the batch's arrays: an
+// item then belongs to one of the sequences that claim it, or to none.
+__device__ __forceinline__ SeqItem find_item(const DevBatch& bt, int item, int unit, int extra,
+                                             int from, int to) {
+  __shared__ int hit, info[5];
   if (threadIdx.x == 0) hit = -1;
   __syncthreads();
-  for (int b = threadIdx.x; b < bt.B; b += threads) {
-    const int lo = min(max(bt.cu[b], 0), bt.n_tokens);
-    const int hi = min(max(bt.cu[b + 1], 0), bt.n_tokens);
-    if (hi > lo && item_base(lo, b, unit, extra) <= item && item < item_base(hi, b + 1, unit, extra))
-      hit = b;
+  SeqItem r;
+  r.b = -1;
+  r.len = 0;
+  r.start = r.all = r.t0 = r.n = 0;
+  for (int b = threadIdx.x; b < bt.B; b += blockDim.x) {
+    const int start = min(max(bt.cu[b], 0), bt.n_tokens), end = min(max(bt.cu[b + 1], 0), bt.n_tokens);
+    const int len = bt.lens[b];
+    const int lo = min(max(start, from), to), hi = min(max(end, from), to);
+    if (hi > lo && item_base(lo - from, b, unit, extra) <= item &&
+        item < item_base(hi - from, b + 1, unit, extra)) {
+      r.b = b;
+      r.t0 = lo;
+      r.n = hi - lo;
+      r.start = start;
+      r.all = end - start;
+      r.len = len;
+      atomicMax(&hit, b);
+    }
   }
   __syncthreads();
-  SeqItem r;
-  r.b = hit;
-  r.first = r.t0 = r.n = 0;
-  if (r.b >= 0) {
-    r.t0 = min(max(bt.cu[r.b], 0), bt.n_tokens);
-    r.n = min(max(bt.cu[r.b + 1], 0), bt.n_tokens) - r.t0;
-    r.first = int(item - item_base(r.t0, r.b, unit, extra));
+  const int found = __builtin_amdgcn_readfirstlane(hit);
+  if (found >= 0 && r.b == found) {
+    info[0] = r.t0;
+    info[1] = r.n;
+    info[2] = r.start;
+    info[3] = r.all;
+    info[4] = int(r.len);
   }
+  __syncthreads();
+  r.b = found;
+  // (without a hit `info` is not set, and nobody reads what follows)
+  // the same in every lane: kept in scalar registers, and so is what follows from them
+  r.t0 = __builtin_amdgcn_readfirstlane(info[0]);
+  r.n = __builtin_amdgcn_readfirstlane(info[1]);
+  r.start = __builtin_amdgcn_readfirstlane(info[2]);
+  r.all = __builtin_amdgcn_readfirstlane(info[3]);
+  r.len = __builtin_amdgcn_readfirstlane(info[4]);
+  r.first = item - item_base(r.t0 - from, r.b, unit, extra);
   return r;
+}
+__device__ __forceinline__ SeqItem find_item(const DevBatch& bt, int item, int unit, int extra) {
+  return find_item(bt, item, unit, extra, 0, bt.n_tokens);
 }
 
 // 2^(code - 127); code 255, the mark of a group that held a NaN or an infinity, gives an

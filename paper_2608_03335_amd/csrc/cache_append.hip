@@ -270,9 +270,9 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
   const int64_t ih = wg >> 1;
   const int h = int(ih % a.c.H);
   const int P = a.c.page;
-  const SeqItem it = find_item(a.b, ih / a.c.H, P, 2, kThreads);
+  const SeqItem it = find_item(a.b, int(ih / a.c.H), P, 2);
   if (it.b < 0) return;
-  const int64_t len = a.b.lens[it.b];
+  const int64_t len = it.len;
   const int64_t start = len - it.n;  // place of the first new token
   const int64_t from = max(start, int64_t(0));
   const int64_t to = min(len, int64_t(a.b.max_pages) * P);
@@ -509,7 +509,7 @@ hipError_t launch_cache_append(const DevCache& c, const DevBatch& b, int d, cons
   a.v_stride = v_stride;
   a.q_stride = q_stride;
   a.Hq = Hq;
-  a.page_wgs = item_base(b.n_tokens, b.B, c.page, 2) * c.H * 2;
+  a.page_wgs = int64_t(item_base(b.n_tokens, b.B, c.page, 2)) * c.H * 2;
   const int64_t units = q ? int64_t(b.n_tokens) * Hq * (d / 16) : 0;
   const int64_t wgs = a.page_wgs + (units + kThreads - 1) / kThreads;
   if (d == 128) return c.fp4 ? append<128, true>(a, wgs, s) : append<128, false>(a, wgs, s);

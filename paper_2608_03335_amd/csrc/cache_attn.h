@@ -5,6 +5,12 @@
 
 namespace spade {
 
+// What the join of a tile's splits has to know, written by the first split.
+struct JoinHead {
+  int splits;                // 0: no such tile, 1: its result is written
+  int t0, nq, head0, heads;  // first token, tokens, first query head, query heads
+};
+
 struct AttnArgs {
   DevCache c;
   DevBatch b;
@@ -17,8 +23,11 @@ struct AttnArgs {
   int causal;
   __bf16* o;
   float* lse;
+  JoinHead* join;
   float* part;              // partial results (splits > 1)
+  int64_t items;            // tiles of all sequences, at most
   int splits;               // most workgroups that share a tile's walk
+  int wgs;                  // workgroups a call is split into, about
 };
 
 // Many queries a sequence: tiles of 128 rows that share staged keys (cache_chunk.hip).
@@ -35,13 +44,13 @@ struct Seen {
   int first, step, len;
   __device__ __forceinline__ int of(int i) const { return min(max(first + i * step, 0), len); }
 };
-__device__ __forceinline__ Seen seen_of(const AttnArgs& a, int b, int n) {
-  const int64_t raw = a.b.lens[b];
+__device__ __forceinline__ Seen seen_of(const AttnArgs& a, const SeqItem& it) {
+  const int64_t raw = it.len;
   Seen s;
   s.len = int(min(max(raw, int64_t(0)), int64_t(a.b.max_pages) * a.c.page));
   s.step = a.causal;
   // a context of fewer tokens than are new leaves the first ones nothing to see
-  s.first = a.causal ? int(max(raw - n + 1, int64_t(-(1 << 30)))) : s.len;
+  s.first = a.causal ? int(max(raw - it.n + 1, int64_t(-(1 << 30)))) : s.len;
   return s;
 }
 #endif

@@ -30,10 +30,14 @@ constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kMaxSplits = 64;
 constexpr int kMinUnits = 16;      // units a split is worth: its start and join cost as much
-constexpr int kTargetWgs = 2048;   // workgroups a call is split into, about
+// Workgroups that are on the card at once (256 CUs, by registers): a call is split into about
+// as many. On 64 4-bit contexts of up to 16384 tokens: 384 186 us, 512 183, 768 175, 1024 177,
+// 2048 200; two of 131072 in bf16: 384 108, 512 106, 768 and more 117.
+template <int D, bool FP4>
+constexpr int target_wgs() { return 256 * (D == 128 && !FP4 ? 2 : 3); }
 constexpr float kLazy = 8.0f;      // the running maximum is raised when a row's grew by 2^8
 
-// What a work item covers; the same in the attention and in the join.
+// What a work item covers.
 struct Tile {
   int b, t0, nq;        // sequence, first token, tokens
   int h, head0, heads;  // K/V head, first query head, query heads of the tile
@@ -46,7 +50,9 @@ __device__ __forceinline__ int tile_walk(const AttnArgs& a, int pages) {  // pag
   return a.topk ? int(min(int64_t(a.topk) * a.QT, int64_t(pages))) : pages;
 }
 
-__device__ __forceinline__ bool find_tile(const AttnArgs& a, Tile* t) {
+// Workgroups are numbered with the heads running fastest, then the tiles, then the splits:
+// the XCDs, which take them in turn, get equal shares of every sequence.
+__device__ __forceinline__ bool find_tile(const AttnArgs& a, int tile, int y, Tile* t) {
   // all units of the call, for the splits' size
   __shared__ unsigned long long total;
   if (threadIdx.x == 0) total = 0;
@@ -61,24 +67,27 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& a, Tile* t) {
     }
     if (mine) atomicAdd(&total, mine);
   }
-  const SeqItem it = find_item(a.b, blockIdx.x, a.QT, a.QT > 1, kThreads);
+  const SeqItem it = find_item(a.b, tile, a.QT, a.QT > 1);
   if (it.b < 0) return false;
   const int skip = it.first * a.QT;
   if (skip >= it.n) return false;
   t->b = it.b;
   t->t0 = it.t0 + skip;
   t->nq = min(a.QT, it.n - skip);
-  t->h = blockIdx.y / a.RT;
-  const int r0 = (blockIdx.y - t->h * a.RT) * 16;
+  t->h = y / a.RT;
+  const int r0 = (y - t->h * a.RT) * 16;
   t->head0 = t->h * a.G + r0;
   t->heads = min(a.G - r0, 16);
-  t->seen = seen_of(a, it.b, it.n);
+  t->seen = seen_of(a, it);
   t->seen.first += skip * t->seen.step;
   t->pages = (t->seen.of(t->nq - 1) + P - 1) / P;
   t->splits = 1;
   if (a.splits > 1) {
     const int64_t upp = P >> 5, units = tile_walk(a, t->pages) * upp;
-    const int64_t even = (int64_t(total) * upp * gridDim.y + kTargetWgs - 1) / kTargetWgs;
+    const uint64_t all = total;
+    const int64_t sum = int64_t(uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(all >> 32))) << 32 |
+                                __builtin_amdgcn_readfirstlane(uint32_t(all)));
+    const int64_t even = (sum * upp * (a.c.H * a.RT) + a.wgs - 1) / a.wgs;
     const int64_t size = max(even, int64_t(kMinUnits));
     t->splits = int(min(max((units + size - 1) / size, int64_t(1)), int64_t(a.splits)));
   }
@@ -313,10 +322,9 @@ __device__ __forceinline__ int build_list(const AttnArgs& a, const Tile& t, uint
 
 // Four channels of a finished row.
 template <int D>
-__device__ __forceinline__ void write_row(const AttnArgs& a, const Tile& t, int rq, int gh, int c4,
-                                          cf32x4 x, float top, float sum) {
+__device__ __forceinline__ void write_row(const AttnArgs& a, int64_t orow, int c4, cf32x4 x, float top,
+                                          float sum) {
   const float inv = top == kNegInf ? 0.0f : 1.0f / sum;
-  const int64_t orow = int64_t(t.t0 + rq) * a.Hq + t.head0 + gh;
   cu32x2 y;
   y[0] = __builtin_bit_cast(uint32_t, __builtin_convertvector(cf32x2{x[0] * inv, x[1] * inv}, cbf16x2));
   y[1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(cf32x2{x[2] * inv, x[3] * inv}, cbf16x2));
@@ -330,10 +338,15 @@ __global__ void __launch_bounds__(kThreads, FP4 ? 3 : 2) cache_attn_kernel(AttnA
   constexpr int OROW = D + 4;  // fp32 row of the waves' merge in LDS
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float ml[kWaves][16][2];
+  const int ny = a.c.H * a.RT;
+  const int per = int(a.items), y = blockIdx.x % ny;
+  const int split = blockIdx.x / ny / per, tile = blockIdx.x / ny % per;
   Tile t;
-  if (!find_tile(a, &t)) return;
-  const int split = blockIdx.z;
-  if (split >= t.splits) return;
+  const bool any = find_tile(a, tile, y, &t);
+  if (a.splits > 1 && split == 0 && threadIdx.x == 0)
+    a.join[int64_t(tile) * ny + y] =
+        any ? JoinHead{t.splits, t.t0, t.nq, t.head0, t.heads} : JoinHead{0, 0, 0, 0, 0};
+  if (!any || split >= t.splits) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int P = a.c.page, upp = P >> 5;
@@ -341,7 +354,7 @@ __global__ void __launch_bounds__(kThreads, FP4 ? 3 : 2) cache_attn_kernel(AttnA
   load_q(a, t, lane, w);
   uint32_t* list = (uint32_t*)lds;  // entries: page << 16 | tokens of the tile that keep it
   int entries = t.pages;
-  if (a.topk) entries = build_list(a, t, list);
+  if (a.topk) entries = __builtin_amdgcn_readfirstlane(build_list(a, t, list));
   const int units = entries * upp;
   const int u0 = int(int64_t(units) * split / t.splits), u1 = int(int64_t(units) * (split + 1) / t.splits);
 
@@ -432,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, FP4 ? 3 : 2) cache_attn_kernel(AttnA
     for (int c = 0; c < CT; ++c)
       *(cf32x4*)(osum + (wave * 16 + r) * OROW + c * 16 + g * 4) = w.o[c] * f;
     __syncthreads();
-    const int64_t slot = (int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * a.splits + split;
+    const int64_t slot = (int64_t(tile) * ny + y) * a.splits + split;
     float* po = a.part + slot * (16 * D + 32);
     for (int i = tid; i < 16 * (D / 4); i += kThreads) {
       const int row = i / (D / 4), c4 = i % (D / 4);
@@ -454,7 +467,7 @@ __global__ void __launch_bounds__(kThreads, FP4 ? 3 : 2) cache_attn_kernel(AttnA
           po[16 * D + row * 2 + 1] = sum;
         }
       } else {
-        write_row<D>(a, t, rq, gh, c4, x, top, sum);
+        write_row<D>(a, int64_t(t.t0 + rq) * a.Hq + t.head0 + gh, c4, x, top, sum);
       }
     }
     if (only < 0) break;
@@ -467,13 +480,13 @@ template <int D>
 __global__ void __launch_bounds__(kThreads) cache_join_kernel(AttnArgs a) {
   constexpr int PIECES = D / 4, RUNS = 64 / PIECES;
   constexpr int64_t STRIDE = 16 * D + 32;
-  Tile t;
-  if (!find_tile(a, &t) || t.splits <= 1) return;
+  const JoinHead t = a.join[blockIdx.x];
+  if (t.splits <= 1) return;
   const int lane = threadIdx.x & 63, c4 = lane % PIECES, run = lane / PIECES;
-  const int row = blockIdx.z * kWaves + (threadIdx.x >> 6);
+  const int row = blockIdx.y * kWaves + (threadIdx.x >> 6);
   const int rq = row / t.heads, gh = row - rq * t.heads;
   if (rq >= t.nq) return;
-  const float* po = a.part + (int64_t(blockIdx.x) * gridDim.y + blockIdx.y) * a.splits * STRIDE;
+  const float* po = a.part + int64_t(blockIdx.x) * a.splits * STRIDE;
   static_assert(kMaxSplits <= 64, "a lane holds one split's statistics");
   const bool in = lane < t.splits;
   const float m = in ? po[lane * STRIDE + 16 * D + row * 2] : kNegInf;
@@ -486,7 +499,7 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(AttnArgs a) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
   cf32x4 x{};
-#pragma unroll 4
+#pragma unroll 8
   for (int s0 = 0; s0 < t.splits; s0 += RUNS) {
     const int s = min(s0 + run, t.splits - 1);
     const float fs = __shfl(f, s);
@@ -497,12 +510,12 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(AttnArgs a) {
   for (int o = PIECES; o < 64; o <<= 1)
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] += __shfl_xor(x[i], o);
-  if (run == 0) write_row<D>(a, t, rq, gh, c4, x, top, sum);
+  if (run == 0) write_row<D>(a, int64_t(t.t0 + rq) * a.Hq + t.head0 + gh, c4, x, top, sum);
 }
 
 struct Plan {
   bool chunk;
-  int G, QT, RT, splits;
+  int G, QT, RT, splits, wgs;
   int64_t items;
   int lds;
 };
@@ -514,6 +527,8 @@ Plan plan(const DevCache& c, const DevBatch& b, int d, int Hq, int topk) {
   p.RT = (p.G + 15) / 16;
   p.items = p.QT > 1 ? item_base(b.n_tokens, b.B, p.QT, 1) : b.n_tokens;
   p.splits = 1;
+  p.wgs = d == 128 ? (c.fp4 ? target_wgs<128, true>() : target_wgs<128, false>())
+                   : (c.fp4 ? target_wgs<64, true>() : target_wgs<64, false>());
   // many rows a sequence: tiles of 128 rows share their keys, where they fill the card
   const int64_t rows = int64_t(b.n_tokens) * p.G;
   p.chunk = p.G <= 32 && rows >= int64_t(b.B) * 64 && rows / 128 * c.H >= 128;
@@ -524,7 +539,7 @@ Plan plan(const DevCache& c, const DevBatch& b, int d, int Hq, int topk) {
   int64_t walk = b.max_pages;
   const int64_t each = (int64_t(b.n_tokens) + b.B - 1) / b.B;  // tokens a sequence, on average
   if (topk && topk * (each < p.QT ? each : p.QT) < walk) walk = topk * (each < p.QT ? each : p.QT);
-  int64_t s = (2 * kTargetWgs + wgs - 1) / wgs;
+  int64_t s = (2 * p.wgs + wgs - 1) / wgs;
   const int64_t most = (walk * (c.page / 32) + kMinUnits - 1) / kMinUnits;
   s = s < most ? s : most;
   s = s < kMaxSplits ? s : kMaxSplits;
@@ -533,6 +548,8 @@ Plan plan(const DevCache& c, const DevBatch& b, int d, int Hq, int topk) {
   return p;
 }
 
+size_t join_bytes(size_t tiles) { return (tiles * sizeof(JoinHead) + 255) / 256 * 256; }
+
 template <int D, bool FP4>
 hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t s) {
   if (p.lds > 48 * 1024) {
@@ -540,12 +557,12 @@ hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t s) {
                                             kCacheMaxPages * 4 + kWaves * 16 * (D + 4) * 4);
     if (e != hipSuccess) return e;
   }
-  const unsigned ny = unsigned(a.c.H * p.RT);
-  cache_attn_kernel<D, FP4><<<dim3(unsigned(p.items), ny, p.splits), kThreads, p.lds, s>>>(a);
+  const int64_t tiles = p.items * a.c.H * p.RT;
+  cache_attn_kernel<D, FP4><<<dim3(unsigned(tiles * p.splits)), kThreads, p.lds, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   const int rows = p.QT * (p.G < 16 ? p.G : 16);
-  cache_join_kernel<D><<<dim3(unsigned(p.items), ny, (rows + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
+  cache_join_kernel<D><<<dim3(unsigned(tiles), (rows + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -554,7 +571,8 @@ hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t s) {
 size_t cache_attn_workspace_bytes(const DevCache& c, const DevBatch& b, int d, int Hq, int topk) {
   const Plan p = plan(c, b, d, Hq, topk);
   if (p.chunk || p.splits == 1) return 0;
-  return size_t(p.items) * c.H * p.RT * p.splits * (16 * d + 32) * 4;
+  const size_t tiles = size_t(p.items) * c.H * p.RT;
+  return join_bytes(tiles) + tiles * p.splits * (16 * d + 32) * 4;
 }
 
 hipError_t launch_cache_attn(const DevCache& c, const DevBatch& b, int d, const CacheAttn& x,
@@ -575,8 +593,11 @@ hipError_t launch_cache_attn(const DevCache& c, const DevBatch& b, int d, const 
   a.causal = x.causal;
   a.o = (__bf16*)x.o;
   a.lse = x.lse;
-  a.part = (float*)ws;
+  a.join = (JoinHead*)ws;
+  a.part = (float*)((char*)ws + join_bytes(size_t(p.items) * c.H * p.RT));
   a.splits = p.splits;
+  a.items = p.items;
+  a.wgs = p.wgs;
   if (p.chunk) return launch_chunk_attn(a, d, s);
   if (d == 128) return c.fp4 ? run<128, true>(a, p, s) : run<128, false>(a, p, s);
   return c.fp4 ? run<64, true>(a, p, s) : run<64, false>(a, p, s);

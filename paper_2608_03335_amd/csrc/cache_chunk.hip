@@ -9,9 +9,10 @@
 // of a page that only some of its rows keep cost nothing to mask: a row's bias is its
 // running maximum, or infinity where the row does not keep the page.
 //
-// bf16 units go from memory to LDS directly, two units ahead of the computation in a ring
-// of three; 4-bit units are loaded two ahead into registers and widened to bf16 on the way
-// to LDS, once for four waves (V's powers of two are applied there: exact).
+// bf16 units go from memory to LDS directly, into a ring that runs three units ahead of the
+// computation (seven at d = 64): what other workgroups have not yet brought to L2 takes longer than
+// two units' computation. 4-bit units run eight ahead as they lie in the page, and are widened to
+// bf16 one unit ahead, once for four waves (V's powers of two are applied there: exact).
 //
 // S^T (32 keys x 32 rows) = K Q^T and O^T += V^T P^T with mfma 32x32x16. The lane's scores
 // are then in the order in which a V fragment holds its keys. Softmax as in cache_attn.hip;
@@ -32,12 +33,16 @@ constexpr int kRows = 32;          // rows of a wave
 constexpr int kSeg = 512;          // pages walked before the masks are built anew
 constexpr float kLazy = 8.0f;
 
+// LDS of the walk. bf16: a ring of units that are on their way or in use. 4 bits: a ring of
+// units as they lie in the page, and two widened ones.
 template <int D, bool FP4>
 struct Stage {
-  static constexpr int SIDE = 32 * D * 2;  // K or V of a unit in LDS
-  static constexpr int BUFS = FP4 ? 2 : 3;
-  static constexpr int LOADS = SIDE / 1024 / kWaves;  // 1 KB loads a wave and side
-  static constexpr int BYTES = BUFS * 2 * SIDE;
+  static constexpr int SIDE = 32 * D * 2;                // K or V of a unit, bf16
+  static constexpr int WIDE = 2 * SIDE;
+  static constexpr int PAGE = 34 * D;                    // a 4-bit unit with its scales
+  static constexpr int RING = FP4 ? 8 : D == 128 ? 4 : 8;
+  static constexpr int LOADS = FP4 ? 2 : WIDE / 1024 / kWaves;  // a wave's loads of a unit
+  static constexpr int BYTES = FP4 ? 2 * WIDE + RING * PAGE : RING * WIDE;
 };
 
 struct Seg {
@@ -54,13 +59,13 @@ template <int N>
 __device__ __forceinline__ void unit_barrier() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
-__device__ __forceinline__ void lds_barrier() {
-  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-}
 
-// 16 bytes a lane from base + off to LDS address dst + 16 lane.
+// 16 (4) bytes a lane from base + off to LDS address dst + 16 (4) lane.
 __device__ __forceinline__ void to_lds(const void* base, uint32_t off, uint32_t dst) {
   asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "{m0}"(dst) : "memory");
+}
+__device__ __forceinline__ void to_lds4(const void* base, uint32_t off, uint32_t dst) {
+  asm volatile("global_load_lds_dword %0, %1" ::"v"(off), "s"(base), "{m0}"(dst) : "memory");
 }
 
 template <typename T>
@@ -69,34 +74,6 @@ __device__ __forceinline__ const T* uniform(const T* p) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(x));
   const uint32_t hi = __builtin_amdgcn_readfirstlane(uint32_t(x >> 32));
   return reinterpret_cast<const T*>(uint64_t(hi) << 32 | lo);
-}
-
-// A 4-bit unit on its way: this thread's share.
-template <int D>
-struct Raw {
-  cu32x2 k, v, vs;
-  uint32_t ks;
-};
-
-template <int D>
-__device__ __forceinline__ void load_raw(const DevCache& c, int64_t base, int kb, int tid, Raw<D>& r) {
-  const uint8_t* kp = (const uint8_t*)c.k + (base >> 1) + kb * 16 * D;
-  const uint8_t* vp = (const uint8_t*)c.v + (base >> 1) + kb * 16 * D;
-  const uint8_t* ks = c.ks + (base >> 5) + kb * D;
-  const uint8_t* vs = c.vs + (base >> 5) + kb * D;
-  const int tile = tid >> 7, g = (tid >> 5) & 3, m = (tid >> 1) & 15;
-  if constexpr (D == 128) {
-    r.k = ((const cu32x2*)kp)[tid];
-    r.v = ((const cu32x2*)vp)[tid];
-    r.ks = ks[tile * 64 + g * 16 + m];
-    const int gr = (tid >> 7) * 2 + (tid & 1);  // column tiles 4 half + 2 (tid & 1) + {0, 1}
-    r.vs = ((const cu32x2*)vs)[g * 4 + gr];
-  } else {
-    r.k[0] = ((const uint32_t*)kp)[tid];
-    r.v[0] = ((const uint32_t*)vp)[tid];
-    r.ks = ks[tile * 32 + (g >> 1) * 16 + m];
-    r.vs = ((const cu32x2*)vs)[(tid >> 6) * 2 + ((tid & 3) >> 1)];
-  }
 }
 
 __device__ __forceinline__ cbf16x8 scaled_eight(uint32_t x, cu32x2 scales) {
@@ -113,28 +90,30 @@ __device__ __forceinline__ cbf16x8 scaled_eight(uint32_t x, cu32x2 scales) {
   return y;
 }
 
+// Widens a 4-bit unit: each thread 2 D / 256 dwords of either side, 8 values a dword.
 template <int D>
-__device__ __forceinline__ void store_raw(const Raw<D>& r, char* buf, int tid) {
-  const int tile = tid >> 7, g = (tid >> 5) & 3, m = (tid >> 1) & 15;
+__device__ __forceinline__ void widen(const char* raw, char* buf, int tid) {
   constexpr int W = D / 64;  // dwords a thread and side
-  const float s = scale_of(r.ks);
+  typedef uint32_t words __attribute__((ext_vector_type(W == 2 ? 2 : 1)));
+  const words k = ((const words*)raw)[tid], v = ((const words*)(raw + 16 * D))[tid];
+  const uint8_t* ks = (const uint8_t*)raw + 32 * D;
+  const uint8_t* vs = ks + D;
+  const int tile = tid >> 7, g = (tid >> 5) & 3, m = (tid >> 1) & 15;
+  const float s = scale_of(ks[tile * (D / 2) + (D == 128 ? g : g >> 1) * 16 + m]);
 #pragma unroll
   for (int i = 0; i < W; ++i) {
     const int ch = g * (D / 4) + ((tid & 1) * W + i) * 8;  // first of 8 channels
     *(cbf16x8*)(buf + ((tile * (D / 32) + (ch >> 5)) * 64 + ((ch & 31) >> 3) * 16 + m) * 16) =
-        fp4_eight(r.k[i], s);
+        fp4_eight(k[i], s);
   }
   char* vb = buf + Stage<D, true>::SIDE;
-  if constexpr (D == 128) {
+  // D = 128: column tiles 4 half + 2 (tid & 1) + {0, 1} of lane group g; D = 64: tile tid & 3
+  const int ct = D == 128 ? tile * 4 + (tid & 1) * 2 : tid & 3;
+  const int vg = D == 128 ? g : tid >> 6, vm = D == 128 ? m : (tid >> 2) & 15;
+  const cu32x2 two = ((const cu32x2*)vs)[vg * (D / 32) + (ct >> 1)];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int ct = (tid >> 7) * 4 + (tid & 1) * 2 + i;
-      *(cbf16x8*)(vb + ((ct * 4 + g) * 16 + m) * 16) = scaled_eight(r.v[i], r.vs);
-    }
-  } else {
-    const int ct = tid & 3;
-    *(cbf16x8*)(vb + ((ct * 4 + (tid >> 6)) * 16 + ((tid >> 2) & 15)) * 16) = scaled_eight(r.v[0], r.vs);
-  }
+  for (int i = 0; i < W; ++i)
+    *(cbf16x8*)(vb + (((ct + i) * 4 + vg) * 16 + vm) * 16) = scaled_eight(v[i], two);
 }
 
 __device__ __forceinline__ float row_max(float v) {  // over the two lanes of a row
@@ -216,12 +195,12 @@ __global__ void __launch_bounds__(kThreads, 2) cache_chunk_kernel(AttnArgs a, in
   const int64_t slot = blockIdx.x >> 3, L = (blockIdx.x & 7) * per + slot;
   if (slot >= per || L >= total) return;
   const int h = int(L / items);
-  const SeqItem it = find_item(a.b, L - h * items, a.QT, 1, kThreads);
+  const SeqItem it = find_item(a.b, int(L - h * items), a.QT, 1);
   if (it.b < 0) return;
   const int skip = it.first * a.QT;
   if (skip >= it.n) return;
   const int t0 = it.t0 + skip, nq = min(a.QT, it.n - skip);
-  Seen seen = seen_of(a, it.b, it.n);
+  Seen seen = seen_of(a, it);
   seen.first += skip * seen.step;
   const int P = a.c.page, upp = P >> 5;
   const int pages = (seen.of(nq - 1) + P - 1) / P;
@@ -301,65 +280,65 @@ __global__ void __launch_bounds__(kThreads, 2) cache_chunk_kernel(AttnArgs a, in
       __syncthreads();
       const int units = base_n * upp;
 
-      // the cursor of the loads: two units ahead of the computation
-      int le = 0, lkb = 0;
-      auto page_base = [&](int e) {
-        return (int64_t(__builtin_amdgcn_readfirstlane(sg.phys[e])) * a.c.H + h) * P * D;
-      };
-      auto advance = [&] {
+      // the cursor of the loads
+      int le = 0, lkb = 0, lbuf = 0;
+      auto fetch = [&] {
+        const int64_t base = (int64_t(__builtin_amdgcn_readfirstlane(sg.phys[le])) * a.c.H + h) * P * D +
+                             lkb * (32 * D);
+        if constexpr (FP4) {  // a quarter of the unit a wave: K, K, V, V, and so with the scales
+          const bool k = wave < 2;
+          const uint32_t dst = lds0 + 2 * ST::WIDE + lbuf * ST::PAGE, part = wave & 1;
+          const uint8_t* data = uniform((const uint8_t*)(k ? a.c.k : a.c.v) + (base >> 1) + part * (8 * D));
+          const uint8_t* scale = uniform((k ? a.c.ks : a.c.vs) + (base >> 5) + part * (D / 2));
+          if (D == 128 || lane < 32) to_lds(data, lane * 16, dst + wave * (8 * D));
+          if (lane < D / 8) to_lds4(scale, lane * 4, dst + 32 * D + wave * (D / 2));
+        } else {
+          const char* kp = (const char*)uniform((const __bf16*)a.c.k + base);
+          const char* vp = (const char*)uniform((const __bf16*)a.c.v + base);
+          const uint32_t dst = lds0 + lbuf * ST::WIDE;
+#pragma unroll
+          for (int i = 0; i < ST::LOADS / 2; ++i) {
+            const uint32_t off = (wave * (ST::LOADS / 2) + i) * 1024;
+            to_lds(kp, off + lane * 16, dst + off);
+            to_lds(vp, off + lane * 16, dst + ST::SIDE + off);
+          }
+        }
+        lbuf = lbuf + 1 == ST::RING ? 0 : lbuf + 1;
         if (++lkb == upp) lkb = 0, ++le;
       };
-      auto fetch = [&](int buf) {  // bf16
-        const int64_t base = page_base(le) + lkb * (32 * D);
-        const char* kp = (const char*)uniform((const __bf16*)a.c.k + base);
-        const char* vp = (const char*)uniform((const __bf16*)a.c.v + base);
-        const uint32_t dst = lds0 + buf * 2 * ST::SIDE;
-#pragma unroll
-        for (int i = 0; i < ST::LOADS; ++i) {
-          const uint32_t off = (wave * ST::LOADS + i) * 1024;
-          to_lds(kp, off + lane * 16, dst + off);
-          to_lds(vp, off + lane * 16, dst + ST::SIDE + off);
-        }
-        advance();
-      };
-      Raw<D> raw;
-      auto fetch_raw = [&] {
-        load_raw<D>(a.c, page_base(le), lkb, tid, raw);
-        advance();
-      };
+      // bf16: unit u + RING - 1 is asked for when unit u begins; 4 bits: unit u + RING, while
+      // unit u + 1 is widened
+      constexpr int AHEAD = FP4 ? ST::RING : ST::RING - 1;
+      for (int u = 0; u < min(units, AHEAD); ++u) fetch();
       if constexpr (FP4) {
-        if (units > 0) {
-          fetch_raw();
-          store_raw<D>(raw, lds, tid);
-          if (units > 1) fetch_raw();
-        }
-      } else {
-        if (units > 0) fetch(0);
-        if (units > 1) fetch(1);
+        if (units >= AHEAD) unit_barrier<(AHEAD - 1) * ST::LOADS>();
+        else unit_barrier<0>();
+        if (units > 0) widen<D>(lds + 2 * ST::WIDE, lds, tid);
       }
-      int e = 0, kb = 0, buf = 0;
+      int e = 0, kb = 0, buf = 0, raw = 0;
       for (int u = 0; u < units; ++u) {
+        // what is needed now has landed: later units may be on their way
+        constexpr int FLIGHT = (AHEAD - (FP4 ? 2 : 1)) * ST::LOADS;
+        if (u + AHEAD <= units) unit_barrier<FLIGHT>();
+        else unit_barrier<0>();
+        if (u + AHEAD < units) fetch();
         if constexpr (FP4) {
-          lds_barrier();
-          if (u + 1 < units) store_raw<D>(raw, lds + (buf ^ 1) * 2 * ST::SIDE, tid);
-          if (u + 2 < units) fetch_raw();
-        } else {
-          if (u + 1 < units) unit_barrier<2 * ST::LOADS>();
-          else unit_barrier<0>();
-          if (u + 2 < units) fetch(buf == 0 ? 2 : buf - 1);
+          raw = raw + 1 == ST::RING ? 0 : raw + 1;
+          if (u + 1 < units)
+            widen<D>(lds + 2 * ST::WIDE + raw * ST::PAGE, lds + (buf ^ 1) * ST::WIDE, tid);
         }
         const int page = sg.page[e];
         const uint32_t who = (a.topk ? __builtin_amdgcn_readfirstlane(sg.mask[wave][page]) : all) & ours;
         const int at = (seg0 + __builtin_amdgcn_readfirstlane(page)) * P + kb * 32;
         if (who && at < most) {
-          const char* kf = lds + buf * 2 * ST::SIDE + kf_lane;
-          const char* vf = lds + buf * 2 * ST::SIDE + ST::SIDE + vf_lane;
+          const char* kf = lds + buf * ST::WIDE + kf_lane;
+          const char* vf = lds + buf * ST::WIDE + ST::SIDE + vf_lane;
           const bool row_in = live && (who >> qi & 1);
           if (at + 32 <= least) step<D, false>(kf, vf, w, lane, a.scale2, at, row_seen, row_in, most);
           else step<D, true>(kf, vf, w, lane, a.scale2, at, row_seen, row_in, most);
         }
         if (++kb == upp) kb = 0, ++e;
-        buf = buf + 1 == ST::BUFS ? 0 : buf + 1;
+        buf = buf + 1 == (FP4 ? 2 : ST::RING) ? 0 : buf + 1;
       }
     }
     if (only < 0 && QW > 1) {
