@@ -46,11 +46,10 @@ struct Stage {
 };
 
 struct Seg {
-  uint32_t mask[kWaves][kSeg];  // tokens of the wave that keep the page
+  uint32_t mask[kWaves][kSeg];  // tokens of the wave that keep page i, then entry i of the walk
   int phys[kSeg];               // kept pages in ascending order
-  uint16_t page[kSeg];          // their place in the segment
+  int page[kSeg];               // their place in the sequence
   int wave_n[2][kWaves];
-  int n;
 };
 
 // Barrier behind which every wave has at most N loads to LDS in flight and has read what it
@@ -128,21 +127,37 @@ struct Rows {
   float m, l;
 };
 
-// One staged unit, keys at..at+31. row_in: the lane's row keeps the page. EDGE: a row sees the
-// keys below row_seen, and V is cleared from key v_seen on.
-template <int D, bool EDGE>
+// One staged unit, keys at..at+31. row_in: the lane's row keeps the page. edge (the same for all
+// lanes): a row sees the keys below row_seen, and V is cleared from key v_seen on. One path for
+// both, with the masks as side steps: two would hold two sets of accumulators.
+template <int D>
 __device__ __forceinline__ void step(const char* kf, const char* vf, Rows<D>& w, int lane, float scale2,
-                                     int at, int row_seen, bool row_in, int v_seen) {
-  const int half = lane >> 5;
+                                     int at, bool edge, int row_seen, bool row_in, int v_seen) {
+  const int key0 = at + 4 * (lane >> 5);  // the lane's keys: key0 + {0..3, 8..11, 16..19, 24..27}
+  cbf16x8 k[D / 16];
+  cu32x4 v[D / 32][2];
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) k[i] = *(const cbf16x8*)(kf + (i >> 1) * 1024 + (i & 1) * 512);
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) v[c][t] = *(const cu32x4*)(vf + c * 2048 + t * 512);
+  __builtin_amdgcn_sched_barrier(0);  // all reads first: else each waits just before its use
   f32x16 s = {};
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k)
-    s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-        *(const cbf16x8*)(kf + (k >> 1) * 1024 + (k & 1) * 512), w.q[k], s, 0, 0, 0);
-  if constexpr (EDGE) {
+  for (int i = 0; i < D / 16; ++i) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[i], w.q[i], s, 0, 0, 0);
+  if (edge) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      s[i] = at + 8 * (i >> 2) + 4 * half + (i & 3) < row_seen ? s[i] : kNegInf;
+    for (int i = 0; i < 16; ++i) s[i] = key0 + 8 * (i >> 2) + (i & 3) < row_seen ? s[i] : kNegInf;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int key = key0 + 8 * t + (i >> 1) * 16 + (i & 1) * 2;
+        const uint32_t keep = (key < v_seen ? 0xffffu : 0u) | (key + 1 < v_seen ? 0xffff0000u : 0u);
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) v[c][t][i] &= keep;
+      }
   }
   float top = fmaxf(s[0], s[1]);
 #pragma unroll
@@ -170,19 +185,10 @@ __device__ __forceinline__ void step(const char* kf, const char* vf, Rows<D>& w,
   }
   w.l += sum;
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c)
+  for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      cbf16x8 f = *(const cbf16x8*)(vf + c * 2048 + t * 512);
-      if constexpr (EDGE) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int key = at + (i >> 2) * 16 + (2 * t + half) * 4 + (i & 3);
-          f[i] = key < v_seen ? f[i] : (__bf16)0.0f;
-        }
-      }
-      w.o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p[t], w.o[c], 0, 0, 0);
-    }
+    for (int c = 0; c < D / 32; ++c)
+      w.o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(cbf16x8, v[c][t]), p[t], w.o[c], 0, 0, 0);
 }
 
 template <int D, bool FP4>
@@ -254,37 +260,44 @@ __global__ void __launch_bounds__(kThreads, 2) cache_chunk_kernel(AttnArgs a, in
         }
         __syncthreads();
       }
-      // the pages that count, in order
-      int base_n = 0;
+      // the pages that count, in order (an entry's place is not behind its page's: in place)
+      int n = 0;
 #pragma unroll
       for (int round = 0; round < kSeg / kThreads; ++round) {
         const int i = round * kThreads + tid;
-        int phys = -1;
-        if (i < span && (!a.topk || (sg.mask[0][i] | sg.mask[1][i] | sg.mask[2][i] | sg.mask[3][i])))
-          phys = table[seg0 + i];
+        uint32_t keep[kWaves];
+        uint32_t any = a.topk ? 0 : 1;
+        if (a.topk)
+#pragma unroll
+          for (int v = 0; v < kWaves; ++v) any |= keep[v] = sg.mask[v][i];
+        const int phys = i < span && any ? table[seg0 + i] : -1;
         const bool ok = phys >= 0 && phys < a.c.n_pages;
         const uint64_t bits = __ballot(ok);
         if (lane == 0) sg.wave_n[round][wave] = __popcll(bits);
         __syncthreads();
-        int at = base_n + __popcll(bits & ((uint64_t(1) << lane) - 1));
+        int at = n + __popcll(bits & ((uint64_t(1) << lane) - 1));
 #pragma unroll
         for (int v = 0; v < kWaves; ++v) {
-          at += v < wave ? sg.wave_n[round][v] : 0;
-          base_n += sg.wave_n[round][v];
+          const int x = __builtin_amdgcn_readfirstlane(sg.wave_n[round][v]);
+          at += v < wave ? x : 0;
+          n += x;
         }
         if (ok) {
           sg.phys[at] = phys;
-          sg.page[at] = uint16_t(i);
+          sg.page[at] = seg0 + i;
+          if (a.topk)
+#pragma unroll
+            for (int v = 0; v < kWaves; ++v) sg.mask[v][at] = keep[v];
         }
       }
       __syncthreads();
-      const int units = base_n * upp;
+      const int units = n * upp;
 
-      // the cursor of the loads
-      int le = 0, lkb = 0, lbuf = 0;
+      // The cursors of the loads and of the computation know the next entry before they need
+      // it: a read of LDS takes as long as four matrix instructions.
+      int le = 0, lkb = 0, lbuf = 0, phys = sg.phys[0], next_phys = sg.phys[min(1, kSeg - 1)];
       auto fetch = [&] {
-        const int64_t base = (int64_t(__builtin_amdgcn_readfirstlane(sg.phys[le])) * a.c.H + h) * P * D +
-                             lkb * (32 * D);
+        const int64_t base = (int64_t(__builtin_amdgcn_readfirstlane(phys)) * a.c.H + h) * P * D + lkb * (32 * D);
         if constexpr (FP4) {  // a quarter of the unit a wave: K, K, V, V, and so with the scales
           const bool k = wave < 2;
           const uint32_t dst = lds0 + 2 * ST::WIDE + lbuf * ST::PAGE, part = wave & 1;
@@ -304,7 +317,12 @@ __global__ void __launch_bounds__(kThreads, 2) cache_chunk_kernel(AttnArgs a, in
           }
         }
         lbuf = lbuf + 1 == ST::RING ? 0 : lbuf + 1;
-        if (++lkb == upp) lkb = 0, ++le;
+        if (++lkb == upp) {
+          lkb = 0;
+          ++le;
+          phys = next_phys;
+          next_phys = sg.phys[min(le + 1, kSeg - 1)];
+        }
       };
       // bf16: unit u + RING - 1 is asked for when unit u begins; 4 bits: unit u + RING, while
       // unit u + 1 is widened
@@ -316,6 +334,8 @@ __global__ void __launch_bounds__(kThreads, 2) cache_chunk_kernel(AttnArgs a, in
         if (units > 0) widen<D>(lds + 2 * ST::WIDE, lds, tid);
       }
       int e = 0, kb = 0, buf = 0, raw = 0;
+      int page = sg.page[0], next_page = sg.page[1];
+      uint32_t mask = sg.mask[wave][0], next_mask = sg.mask[wave][1];
       for (int u = 0; u < units; ++u) {
         // what is needed now has landed: later units may be on their way
         constexpr int FLIGHT = (AHEAD - (FP4 ? 2 : 1)) * ST::LOADS;
@@ -327,17 +347,22 @@ __global__ void __launch_bounds__(kThreads, 2) cache_chunk_kernel(AttnArgs a, in
           if (u + 1 < units)
             widen<D>(lds + 2 * ST::WIDE + raw * ST::PAGE, lds + (buf ^ 1) * ST::WIDE, tid);
         }
-        const int page = sg.page[e];
-        const uint32_t who = (a.topk ? __builtin_amdgcn_readfirstlane(sg.mask[wave][page]) : all) & ours;
-        const int at = (seg0 + __builtin_amdgcn_readfirstlane(page)) * P + kb * 32;
+        const uint32_t who = (a.topk ? __builtin_amdgcn_readfirstlane(mask) : all) & ours;
+        const int at = __builtin_amdgcn_readfirstlane(page) * P + kb * 32;
         if (who && at < most) {
           const char* kf = lds + buf * ST::WIDE + kf_lane;
           const char* vf = lds + buf * ST::WIDE + ST::SIDE + vf_lane;
           const bool row_in = live && (who >> qi & 1);
-          if (at + 32 <= least) step<D, false>(kf, vf, w, lane, a.scale2, at, row_seen, row_in, most);
-          else step<D, true>(kf, vf, w, lane, a.scale2, at, row_seen, row_in, most);
+          step<D>(kf, vf, w, lane, a.scale2, at, at + 32 > least, row_seen, row_in, most);
         }
-        if (++kb == upp) kb = 0, ++e;
+        if (++kb == upp) {
+          kb = 0;
+          ++e;
+          page = next_page;
+          mask = next_mask;
+          next_page = sg.page[min(e + 1, kSeg - 1)];
+          next_mask = sg.mask[wave][min(e + 1, kSeg - 1)];
+        }
         buf = buf + 1 == (FP4 ? 2 : ST::RING) ? 0 : buf + 1;
       }
     }
