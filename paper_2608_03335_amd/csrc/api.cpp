@@ -786,7 +786,7 @@ spade_status spade_cache_append(const spade_cache* c, const spade_batch* b, cons
     return fail(SPADE_ERR_INVALID_ARG, "q_out may be q only where q is contiguous");
   if (r.rot && (!r.cos || !r.sin || !aligned16(r.cos) || !aligned16(r.sin)))
     return fail(SPADE_ERR_INVALID_ARG, "rope: cos and sin must be non-null and 16-byte aligned");
-  const int64_t wgs = int64_t(spade::item_base(b->n_tokens, b->B, c->page, 2)) * c->H * 2 +
+  const int64_t wgs = int64_t(spade::item_base(b->n_tokens, b->B, c->page, 2)) * c->H * 5 +
                       (int64_t(b->n_tokens) * Hq * (c->d / 16) + 255) / 256;
   if (wgs > 0x7fffffff) return fail(SPADE_ERR_UNSUPPORTED, "batch too large (n_tokens, heads)");
   return hip_status(spade::launch_cache_append(dc, db, c->d, r, k, k_stride, v, v_stride, q, q_stride,
@@ -810,7 +810,7 @@ spade_status spade_cache_read(const spade_cache* c, const spade_batch* b, int64_
     return fail(SPADE_ERR_INVALID_ARG, "k, v (two tensors), table and lens must be non-null");
   if (!aligned16(k) || !aligned16(v))
     return fail(SPADE_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
-  if (int64_t(b->B) * b->max_pages * c->H * 2 > 0x7fffffff)
+  if (int64_t(b->B) * b->max_pages > 0x7fffffff / (c->H * 2) / ((c->page + 63) / 64))
     return fail(SPADE_ERR_UNSUPPORTED, "batch too large (B * max_pages * H)");
   return hip_status(spade::launch_cache_read(dc, db, c->d, N, k, v, stream), "cache read launch");
 }

@@ -1,13 +1,13 @@
 // Append to the paged cache with the position rotation, and read-back (gfx950).
 //
-// Append. A workgroup owns one page of one K/V head and one side (K or V): it stages the
-// page's tokens as rows in LDS, rotates and rounds the new ones on the way, and writes
-// them out in the page's fragment order, so global reads are whole rows and global writes
-// whole fragments wherever a fragment is all new. Only one workgroup touches a page's
-// bytes, so 4-bit dwords shared with older tokens are merged without atomics. The K side
-// also reads the page's older keys and writes the page's mean key: from the stored values,
-// in fp64, so it is the same however the tokens arrived (one by one, in chunks, rewritten
-// after a rewind). The remaining workgroups of the launch rotate the queries.
+// Append. A workgroup owns the K of one page and head, or 64 tokens of its V: it stages tokens
+// as rows in LDS, rotates and rounds the new ones on the way, and writes them out in the
+// page's fragment order, so global reads are whole rows and global writes whole fragments
+// wherever a fragment is all new. Only one workgroup touches a page's bytes, so 4-bit dwords
+// shared with older tokens are merged without atomics. The K side also reads the page's older
+// keys and writes the page's mean key: from the stored values, in fp64, so it is the same
+// however the tokens arrived (one by one, in chunks, rewritten after a rewind). The remaining
+// workgroups of the launch rotate the queries, two heads a thread.
 //
 // Rotation: a' = a cos - b sin, b' = a sin + b cos in fp32, every product and sum rounded
 // once (no fused multiply-add: the same bits as the elementary operations), then one
@@ -23,6 +23,9 @@ namespace spade {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kHeads = 2;      // heads a thread turns with one load of the tables (4: 1 to 3 us more)
+constexpr int kCuLds = 1024;   // sequences whose offsets a query workgroup keeps in LDS
+constexpr int kPiece = 64;     // tokens of a page in LDS at once
 
 // Rows of a page in LDS: 8 elements of padding keep rows 16-byte aligned and spread the
 // column reads of the V side over the banks.
@@ -53,14 +56,21 @@ __device__ __forceinline__ UnitPlace unit_place(const DevRope& r, int u) {
   return p;
 }
 
-__device__ __forceinline__ Chunk2 rotate_unit(const DevRope& r, Chunk2 x, int u, int pos) {
-#pragma clang fp contract(off)
+// A unit's eight cosines and sines.
+struct Turn {
+  cf32x4 c[2], s[2];
+};
+__device__ __forceinline__ void load_turn(const DevRope& r, int u, int pos, Turn& f) {
   const int64_t at = int64_t(pos) * (r.rot >> 1) + u * 8;
-  float c[8], s[8], v[16];
-  *(cf32x4*)(c) = *(const cf32x4*)(r.cos + at);
-  *(cf32x4*)(c + 4) = *(const cf32x4*)(r.cos + at + 4);
-  *(cf32x4*)(s) = *(const cf32x4*)(r.sin + at);
-  *(cf32x4*)(s + 4) = *(const cf32x4*)(r.sin + at + 4);
+  f.c[0] = *(const cf32x4*)(r.cos + at);
+  f.c[1] = *(const cf32x4*)(r.cos + at + 4);
+  f.s[0] = *(const cf32x4*)(r.sin + at);
+  f.s[1] = *(const cf32x4*)(r.sin + at + 4);
+}
+
+__device__ __forceinline__ Chunk2 rotate_unit(const DevRope& r, Chunk2 x, const Turn& f) {
+#pragma clang fp contract(off)
+  float v[16];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     v[2 * i] = lo_f(x.a[i]);
@@ -71,7 +81,8 @@ __device__ __forceinline__ Chunk2 rotate_unit(const DevRope& r, Chunk2 x, int u,
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float a = r.interleaved ? v[2 * i] : v[i], b = r.interleaved ? v[2 * i + 1] : v[i + 8];
-    const float ac = a * c[i], bs = b * s[i], as = a * s[i], bc = b * c[i];
+    const float c = f.c[i >> 2][i & 3], s = f.s[i >> 2][i & 3];
+    const float ac = a * c, bs = b * s, as = a * s, bc = b * c;
     if (r.interleaved) {
       v[2 * i] = ac - bs;
       v[2 * i + 1] = as + bc;
@@ -104,42 +115,37 @@ __device__ __forceinline__ int group_exponent(float top) {
   return x;
 }
 
-// Code of value x = y 2^e; inv = 2^-e.
-__device__ __forceinline__ uint32_t e2m1(float y, float inv, uint32_t most) {
-  const float a = fabsf(y) * inv;
-  uint32_t c = uint32_t(a > 0.25f) + uint32_t(a >= 0.75f) + uint32_t(a > 1.25f) +
-               uint32_t(a >= 1.75f) + uint32_t(a > 2.5f) + uint32_t(a >= 3.5f) +
-               uint32_t(a > 5.0f);
-  c = min(c, most);
-  return c | (c != 0 && y < 0.0f ? 8u : 0u);
-}
-
 // Quantises 32 channels (16 dwords of bf16 pairs) to 4 dwords of codes; returns the scale byte.
+// The conversion instruction rounds to nearest, ties to even, and saturates.
 __device__ __forceinline__ uint32_t quantise32(const cu32x4 x[4], uint32_t code[4]) {
-  float top = 0.0f;
-  bool bad = false;
+  typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+  u16x2 most = {0, 0};
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float a = fabsf(lo_f(x[i][j])), b = fabsf(hi_f(x[i][j]));
-      bad |= !(a <= 3.4e38f) | !(b <= 3.4e38f);
-      top = fmaxf(top, fmaxf(a, b));
-    }
-  if (bad) {
+    for (int j = 0; j < 4; ++j)
+      most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x[i][j] & 0x7fff7fffu));
+  const float top = __uint_as_float(uint32_t(max(most[0], most[1])) << 16);
+  if (!(top <= 3.4e38f)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) code[i] = 0;
     return 255;
   }
   const int e = group_exponent(top);
-  const float inv = __uint_as_float(uint32_t(127 - e) << 23);  // e in [-126, 126]
-  const uint32_t most = e == 126 ? 5u : 7u;
+  const float two = __uint_as_float(uint32_t(127 + e) << 23);  // e in [-126, 126]
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
+    // (copies: a bit cast of a vector's element reads its first one)
+    const uint32_t w0 = x[i][0], w1 = x[i][1], w2 = x[i][2], w3 = x[i][3];
     uint32_t c = 0;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      c |= (e2m1(lo_f(x[i][j]), inv, most) | e2m1(hi_f(x[i][j]), inv, most) << 4) << (8 * j);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(cbf16x2, w0), two, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(cbf16x2, w1), two, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(cbf16x2, w2), two, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(cbf16x2, w3), two, 3);
+    if (e == 126) {  // 4 2^126 is beyond bf16: codes 6 and 7 become 5
+      const uint32_t high = (c >> 2) & (c >> 1) & 0x11111111u;  // codes with bits 2 and 1 set
+      c = (c & ~(high * 7u)) | high * 5u;
+    }
     code[i] = c;
   }
   return uint32_t(e + 127);
@@ -150,15 +156,17 @@ __device__ __forceinline__ int64_t page_elem(const DevCache& c, int phys, int h)
   return (int64_t(phys) * c.H + h) * c.page * D;
 }
 
-// Tokens [0, n) of a page's K side as rows in LDS (n <= page; whole tiles are read).
+// Tokens [from, n) of a page's K side as rows in LDS, the first at `rows` (from a multiple of
+// 32, n <= page; whole tiles are read).
 template <int D, bool FP4>
-__device__ __forceinline__ void stage_k(const DevCache& c, int phys, int h, int n, __bf16* rows) {
+__device__ __forceinline__ void stage_k(const DevCache& c, int phys, int h, int from, int n, __bf16* rows) {
   constexpr int R = lds_row<D>();
-  const int tiles = (n + 15) >> 4;
+  const int tiles = (n + 15) >> 4, tile0 = from >> 4;
+  rows -= from * R;
   const int64_t base = page_elem<D>(c, phys, h);
   if constexpr (!FP4) {
     const cu32x4* src = (const cu32x4*)((const __bf16*)c.k + base);
-    for (int i = threadIdx.x; i < tiles * 16 * (D / 8); i += kThreads) {
+    for (int i = tile0 * 2 * D + threadIdx.x; i < tiles * 2 * D; i += kThreads) {
       const int m = i & 15, sg = (i >> 4) % (D / 8), tile = i / (2 * D);
       const int r = tile * 16 + m;
       if (r < n) *(cu32x4*)(rows + r * R + sg * 8) = src[i];
@@ -166,7 +174,7 @@ __device__ __forceinline__ void stage_k(const DevCache& c, int phys, int h, int 
   } else {
     const uint8_t* src = (const uint8_t*)c.k + base / 2;
     const uint8_t* sc = c.ks + base / 32;
-    for (int i = threadIdx.x; i < tiles * 16 * (D / 8); i += kThreads) {
+    for (int i = tile0 * 2 * D + threadIdx.x; i < tiles * 2 * D; i += kThreads) {
       // one dword: 8 channels of token (tile, m), lane group g
       const int w = i % (D / 32), gm = i / (D / 32) % 64, tile = i / (2 * D);
       const int g = gm >> 4, m = gm & 15, r = tile * 16 + m;
@@ -180,11 +188,12 @@ __device__ __forceinline__ void stage_k(const DevCache& c, int phys, int h, int 
 
 // The same for the V side.
 template <int D, bool FP4>
-__device__ __forceinline__ void stage_v(const DevCache& c, int phys, int h, int n, __bf16* rows) {
+__device__ __forceinline__ void stage_v(const DevCache& c, int phys, int h, int from, int n, __bf16* rows) {
   constexpr int R = lds_row<D>();
-  const int blocks = (n + 31) >> 5;
+  const int blocks = (n + 31) >> 5, block0 = from >> 5;
+  rows -= from * R;
   const int64_t base = page_elem<D>(c, phys, h);
-  for (int i = threadIdx.x; i < blocks * 4 * D; i += kThreads) {
+  for (int i = block0 * 4 * D + threadIdx.x; i < blocks * 4 * D; i += kThreads) {
     const int kb = i / (4 * D);
     cbf16x8 x;
     int ch, g;
@@ -222,54 +231,71 @@ struct AppendArgs {
   __bf16* q_out;
   int64_t k_stride, v_stride, q_stride;
   int Hq;
-  int64_t page_wgs;  // the first workgroups: 2 per (page item, head)
+  int64_t page_wgs;  // the first workgroups: for each (page item, head) K, then V in pieces
 };
 
 template <int D, bool FP4>
 __global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
   constexpr int R = lds_row<D>();
   constexpr int U = D / 16;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  __bf16* rows = (__bf16*)lds;
+  // one buffer for a piece's rows, the mean's partial sums, and a query workgroup's offsets
+  __shared__ __attribute__((aligned(16))) char lds[kPiece * R * 2];
+  static_assert(sizeof(lds) >= (kCuLds + 1) * sizeof(int) && sizeof(lds) >= 2 * kThreads * sizeof(double), "");
+  __bf16* piece = (__bf16*)lds;
   const int64_t wg = blockIdx.x;
   const int tid = threadIdx.x;
 
-  if (wg >= a.page_wgs) {  // queries
-    const int64_t i = (wg - a.page_wgs) * kThreads + tid;
-    const int64_t row = i / U;
-    const int u = int(i % U);
-    const int64_t t = row / a.Hq;
+  if (wg >= a.page_wgs) {  // queries: a thread turns one unit of kHeads neighbouring heads
+    int* cu_lds = (int*)lds;
+    const bool staged = a.b.B <= kCuLds;
+    if (staged)
+      for (int i = tid; i <= a.b.B; i += kThreads) cu_lds[i] = a.b.cu[i];
+    const int groups = (a.Hq + kHeads - 1) / kHeads;
+    const int64_t first = (wg - a.page_wgs) * kThreads;
+    const int64_t t_first = first / (groups * U);
+    const int i = int(first - t_first * (groups * U)) + tid;
+    const int64_t t = t_first + i / (groups * U);
+    const int u = i % U, h0 = i / U % groups * kHeads;
+    __syncthreads();
     if (t >= a.b.n_tokens) return;
-    const int hq = int(row - t * a.Hq);
-    // the token's place: only needed where the caller gives no positions
-    int64_t place = 0;
-    bool live = true;
-    {
-      int lo = 0, hi = a.b.B;  // last b with cu[b] <= t
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (a.b.cu[mid] <= t) lo = mid; else hi = mid;
-      }
-      const int c0 = a.b.cu[lo], c1 = a.b.cu[lo + 1];
-      live = c0 <= t && t < c1;
-      place = int64_t(a.b.lens[lo]) - c1 + t;
+    int lo = 0, hi = a.b.B;  // the last b with cu[b] <= t
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if ((staged ? cu_lds[mid] : a.b.cu[mid]) <= t) lo = mid; else hi = mid;
     }
-    if (!live) return;  // behind the last sequence: left as it was
-    const int pos = rope_row(a.r, int(t), place);
+    const int c0 = staged ? cu_lds[lo] : a.b.cu[lo], c1 = staged ? cu_lds[lo + 1] : a.b.cu[lo + 1];
+    if (!(c0 <= t && t < c1)) return;  // of no sequence: left as it was
+    const int64_t place = int64_t(a.b.lens[lo]) - c1 + t;
     const UnitPlace p = unit_place(a.r, u);
-    const __bf16* src = a.q + t * a.q_stride + int64_t(hq) * D;
-    Chunk2 x{*(const cu32x4*)(src + p.a), *(const cu32x4*)(src + p.b)};
-    if (p.turn && pos >= 0) x = rotate_unit(a.r, x, u, pos);
-    __bf16* dst = a.q_out + row * D;
-    *(cu32x4*)(dst + p.a) = x.a;
-    *(cu32x4*)(dst + p.b) = x.b;
+    const __bf16* src = a.q + t * a.q_stride + int64_t(h0) * D;
+    __bf16* dst = a.q_out + (t * a.Hq + h0) * D;
+    const int n = min(kHeads, a.Hq - h0);
+    Chunk2 x[kHeads];
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h)
+      if (h < n) x[h] = Chunk2{*(const cu32x4*)(src + h * D + p.a), *(const cu32x4*)(src + h * D + p.b)};
+    const int pos = p.turn ? rope_row(a.r, int(t), place) : -1;
+    if (pos >= 0) {
+      Turn f;
+      load_turn(a.r, u, pos, f);
+#pragma unroll
+      for (int h = 0; h < kHeads; ++h)
+        if (h < n) x[h] = rotate_unit(a.r, x[h], f);
+    }
+#pragma unroll
+    for (int h = 0; h < kHeads; ++h)
+      if (h < n) {
+        *(cu32x4*)(dst + h * D + p.a) = x[h].a;
+        *(cu32x4*)(dst + h * D + p.b) = x[h].b;
+      }
     return;
   }
 
-  const bool vside = wg & 1;
-  const int64_t ih = wg >> 1;
+  const int P = a.c.page, sides = 1 + (P + kPiece - 1) / kPiece;  // K, and V in pieces
+  const int64_t ih = wg / sides;
+  const int side = int(wg - ih * sides);
+  const bool vside = side > 0;
   const int h = int(ih % a.c.H);
-  const int P = a.c.page;
   const SeqItem it = find_item(a.b, int(ih / a.c.H), P, 2);
   if (it.b < 0) return;
   const int64_t len = it.len;
@@ -285,107 +311,100 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
   const int64_t tok0 = it.t0 + (j * P - start);  // new token at row r: tok0 + r
   const int64_t base = page_elem<D>(a.c, phys, h);
 
-  // new tokens to LDS
-  if (!vside) {
-    stage_k<D, FP4>(a.c, phys, h, lo, rows);
-    for (int i = tid; i < (hi - lo) * U; i += kThreads) {
-      const int r = lo + i / U, u = i % U;
-      const int64_t t = tok0 + r;
-      const UnitPlace p = unit_place(a.r, u);
-      const __bf16* src = a.k + t * a.k_stride + int64_t(h) * D;
-      Chunk2 x{*(const cu32x4*)(src + p.a), *(const cu32x4*)(src + p.b)};
-      if (p.turn) {
-        const int pos = rope_row(a.r, int(t), j * P + r);
-        if (pos >= 0) x = rotate_unit(a.r, x, u, pos);
+  // the mean's sums: a thread adds two channels of every SEGS-th row
+  constexpr int PAIRS = D / 2, SEGS = kThreads / PAIRS;
+  const int cp = tid % PAIRS, seg = tid / PAIRS;
+  double s0 = 0.0, s1 = 0.0;
+  const int p_first = vside ? (side - 1) * kPiece : 0, p_end = vside ? p_first + kPiece : hi;
+  for (int p0 = p_first; p0 < p_end; p0 += kPiece) {
+    const int r0 = max(lo, p0), r1 = min(hi, p0 + kPiece);  // the piece's new tokens
+    if (vside && r0 >= r1) return;
+    __bf16* rows = piece - p0 * R;
+    if (!vside) {
+      stage_k<D, FP4>(a.c, phys, h, p0, min(lo, p0 + kPiece), piece);
+      for (int i = tid; i < (r1 - r0) * U; i += kThreads) {
+        const int r = r0 + i / U, u = i % U;
+        const int64_t t = tok0 + r;
+        const UnitPlace p = unit_place(a.r, u);
+        const __bf16* src = a.k + t * a.k_stride + int64_t(h) * D;
+        Chunk2 x{*(const cu32x4*)(src + p.a), *(const cu32x4*)(src + p.b)};
+        if (p.turn) {
+          const int pos = rope_row(a.r, int(t), j * P + r);
+          if (pos >= 0) {
+            Turn f;
+            load_turn(a.r, u, pos, f);
+            x = rotate_unit(a.r, x, f);
+          }
+        }
+        *(cu32x4*)(rows + r * R + p.a) = x.a;
+        *(cu32x4*)(rows + r * R + p.b) = x.b;
       }
-      *(cu32x4*)(rows + r * R + p.a) = x.a;
-      *(cu32x4*)(rows + r * R + p.b) = x.b;
+    } else {
+      for (int i = tid; i < (r1 - r0) * (D / 8); i += kThreads) {
+        const int r = r0 + i / (D / 8), x = i % (D / 8);
+        const __bf16* src = a.v + (tok0 + r) * a.v_stride + int64_t(h) * D;
+        *(cu32x4*)(rows + r * R + x * 8) = *(const cu32x4*)(src + x * 8);
+      }
     }
-  } else {
-    for (int i = tid; i < (hi - lo) * (D / 8); i += kThreads) {
-      const int r = lo + i / (D / 8), x = i % (D / 8);
-      const __bf16* src = a.v + (tok0 + r) * a.v_stride + int64_t(h) * D;
-      *(cu32x4*)(rows + r * R + x * 8) = *(const cu32x4*)(src + x * 8);
-    }
-  }
-  __syncthreads();
+    __syncthreads();
 
-  if constexpr (FP4) {  // codes out (K) or kept in the row's place (V)
-    for (int i = tid; i < (hi - lo) * (D / 32); i += kThreads) {
-      const int r = lo + i / (D / 32), gr = i % (D / 32);
-      cu32x4* row = (cu32x4*)(rows + r * R + gr * 32);
-      cu32x4 x[4];
+    if constexpr (FP4) {  // codes out (K) or kept in the row's place (V)
+      for (int i = tid; i < (r1 - r0) * (D / 32); i += kThreads) {
+        const int r = r0 + i / (D / 32), gr = i % (D / 32);
+        cu32x4* row = (cu32x4*)(rows + r * R + gr * 32);
+        cu32x4 x[4];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) x[w] = row[w];
-      uint32_t code[4];
-      const uint32_t sc = quantise32(x, code);
-      if (!vside) {
-        const int tile = r >> 4, m = r & 15;
-        uint8_t* kp = (uint8_t*)a.c.k + base / 2 + tile * 8 * D;
-        if constexpr (D == 128) {
-          *(cu32x4*)(kp + (gr * 16 + m) * 16) = cu32x4{code[0], code[1], code[2], code[3]};
+        for (int w = 0; w < 4; ++w) x[w] = row[w];
+        uint32_t code[4];
+        const uint32_t sc = quantise32(x, code);
+        if (!vside) {
+          const int tile = r >> 4, m = r & 15;
+          uint8_t* kp = (uint8_t*)a.c.k + base / 2 + tile * 8 * D;
+          if constexpr (D == 128) {
+            *(cu32x4*)(kp + (gr * 16 + m) * 16) = cu32x4{code[0], code[1], code[2], code[3]};
+          } else {
+            *(cu32x2*)(kp + ((2 * gr) * 16 + m) * 8) = cu32x2{code[0], code[1]};
+            *(cu32x2*)(kp + ((2 * gr + 1) * 16 + m) * 8) = cu32x2{code[2], code[3]};
+          }
+          a.c.ks[base / 32 + tile * (D / 2) + gr * 16 + m] = uint8_t(sc);
+          const float s = scale_of(sc);
+#pragma unroll
+          for (int w = 0; w < 4; ++w)  // the stored values, for the mean
+            row[w] = __builtin_bit_cast(cu32x4, fp4_eight(code[w], s));
         } else {
-          *(cu32x2*)(kp + ((2 * gr) * 16 + m) * 8) = cu32x2{code[0], code[1]};
-          *(cu32x2*)(kp + ((2 * gr + 1) * 16 + m) * 8) = cu32x2{code[2], code[3]};
-        }
-        a.c.ks[base / 32 + tile * (D / 2) + gr * 16 + m] = uint8_t(sc);
-        const float s = scale_of(sc);
+          const int kb = r >> 5, g = (r & 15) >> 2, jj = ((r >> 4) & 1) * 4 + (r & 3);
+          a.c.vs[base / 32 + kb * D + (g * (D / 32) + gr) * 8 + jj] = uint8_t(sc);
 #pragma unroll
-        for (int w = 0; w < 4; ++w)  // the stored values, for the mean
-          row[w] = __builtin_bit_cast(cu32x4, fp4_eight(code[w], s));
-      } else {
-        const int kb = r >> 5, g = (r & 15) >> 2, jj = ((r >> 4) & 1) * 4 + (r & 3);
-        a.c.vs[base / 32 + kb * D + (g * (D / 32) + gr) * 8 + jj] = uint8_t(sc);
+          for (int w = 0; w < 4; ++w) {
+            cu32x4 y;  // one code in each 16-bit place
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          cu32x4 y;  // one code in each 16-bit place
-#pragma unroll
-          for (int z = 0; z < 4; ++z)
-            y[z] = ((code[w] >> (8 * z)) & 15u) | ((code[w] >> (8 * z + 4)) & 15u) << 16;
-          row[w] = y;
+            for (int z = 0; z < 4; ++z)
+              y[z] = ((code[w] >> (8 * z)) & 15u) | ((code[w] >> (8 * z + 4)) & 15u) << 16;
+            row[w] = y;
+          }
         }
       }
+      __syncthreads();
     }
-    __syncthreads();
-  }
 
-  if (!vside) {
-    if constexpr (!FP4) {
-      const int t0 = lo >> 4, t1 = (hi + 15) >> 4;
-      cu32x4* dst = (cu32x4*)((__bf16*)a.c.k + base);
-      for (int i = t0 * 2 * D + tid; i < t1 * 2 * D; i += kThreads) {
-        const int m = i & 15, sg = (i >> 4) % (D / 8), r = i / (2 * D) * 16 + m;
-        if (r >= lo && r < hi) dst[i] = *(cu32x4*)(rows + r * R + sg * 8);
+    if (!vside) {
+      if constexpr (!FP4) {
+        cu32x4* dst = (cu32x4*)((__bf16*)a.c.k + base);
+        for (int i = (r0 >> 4) * 2 * D + tid; i < ((r1 + 15) >> 4) * 2 * D; i += kThreads) {
+          const int m = i & 15, sg = (i >> 4) % (D / 8), r = i / (2 * D) * 16 + m;
+          if (r >= r0 && r < r1) dst[i] = *(cu32x4*)(rows + r * R + sg * 8);
+        }
       }
-    }
-    // mean key of the page's tokens [0, hi)
-    constexpr int PAIRS = D / 2, SEGS = kThreads / PAIRS;
-    __shared__ double part[SEGS][D];
-    const int cp = tid % PAIRS, seg = tid / PAIRS;
-    double s0 = 0.0, s1 = 0.0;
-    for (int r = seg; r < hi; r += SEGS) {
-      const uint32_t x = *(const uint32_t*)(rows + r * R + cp * 2);
-      s0 += double(lo_f(x));
-      s1 += double(hi_f(x));
-    }
-    part[seg][cp * 2] = s0;
-    part[seg][cp * 2 + 1] = s1;
-    __syncthreads();
-    if (tid < PAIRS) {
-      s0 = s1 = 0.0;
-#pragma unroll
-      for (int s = 0; s < SEGS; ++s) {
-        s0 += part[s][tid * 2];
-        s1 += part[s][tid * 2 + 1];
+      for (int r = p0 + seg; r < min(hi, p0 + kPiece); r += SEGS) {
+        const uint32_t x = *(const uint32_t*)(rows + r * R + cp * 2);
+        s0 += double(lo_f(x));
+        s1 += double(hi_f(x));
       }
-      // bf16 means halve what a selection reads; it ranks pages by them, no more
-      ((uint32_t*)a.c.mean)[((int64_t(phys) * a.c.H + h) * D >> 1) + tid] =
-          pack(float(s0 / hi), float(s1 / hi));
+      __syncthreads();  // the next piece overwrites the rows
+      continue;
     }
-  } else {
     const uint16_t* codes = (const uint16_t*)rows;
-    const int b0 = lo >> 5, b1 = (hi + 31) >> 5;
-    for (int i = b0 * 4 * D + tid; i < b1 * 4 * D; i += kThreads) {
+    for (int i = (r0 >> 5) * 4 * D + tid; i < ((r1 + 31) >> 5) * 4 * D; i += kThreads) {
       const int kb = i / (4 * D);
       int ch, g;
       if constexpr (!FP4) {
@@ -400,7 +419,7 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const int r = kb * 32 + (e >> 2) * 16 + g * 4 + (e & 3);
-        const bool is_new = r >= lo && r < hi;
+        const bool is_new = r >= r0 && r < r1;
         mask |= uint32_t(is_new) << e;
         x[e] = is_new ? codes[r * R + ch] : uint16_t(0);
       }
@@ -430,6 +449,23 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
       }
     }
   }
+  if (vside) return;
+  // mean key of the page's tokens [0, hi)
+  double(*part)[D] = (double(*)[D])lds;  // [SEGS][D]: the rows are no longer read
+  part[seg][cp * 2] = s0;
+  part[seg][cp * 2 + 1] = s1;
+  __syncthreads();
+  if (tid < PAIRS) {
+    s0 = s1 = 0.0;
+#pragma unroll
+    for (int s = 0; s < SEGS; ++s) {
+      s0 += part[s][tid * 2];
+      s1 += part[s][tid * 2 + 1];
+    }
+    // bf16 means halve what a selection reads; it ranks pages by them, no more
+    ((uint32_t*)a.c.mean)[((int64_t(phys) * a.c.H + h) * D >> 1) + tid] =
+        pack(float(s0 / hi), float(s1 / hi));
+  }
 }
 
 struct ReadArgs {
@@ -440,28 +476,29 @@ struct ReadArgs {
   int64_t N;
 };
 
-// A workgroup copies one page of one head and side: fragments to LDS rows to raster rows.
+// A workgroup copies 64 tokens of a page of one head and side: fragments to LDS rows to raster
+// rows (of larger pieces too few fit a CU: 128 tokens 61 us for 25385 tokens x 8 heads).
 template <int D, bool FP4>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(ReadArgs a) {
   constexpr int R = lds_row<D>();
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  __bf16* rows = (__bf16*)lds;
+  __shared__ __attribute__((aligned(16))) __bf16 rows[kPiece * R];
   const int64_t wg = blockIdx.x;
   const bool vside = wg & 1;
-  const int64_t bj = (wg >> 1) / a.c.H;
-  const int h = int((wg >> 1) - bj * a.c.H);
+  const int P = a.c.page, pieces = (P + kPiece - 1) / kPiece;
+  const int from = int((wg >> 1) % pieces) * kPiece;
+  const int64_t bjh = (wg >> 1) / pieces, bj = bjh / a.c.H;
+  const int h = int(bjh - bj * a.c.H);
   const int b = int(bj / a.b.max_pages), j = int(bj - int64_t(b) * a.b.max_pages);
-  const int P = a.c.page;
   const int64_t to = min(int64_t(a.b.lens[b]), a.N);
-  const int n = int(min(to - int64_t(j) * P, int64_t(P)));
-  if (n <= 0) return;
+  const int n = int(min(to - int64_t(j) * P, int64_t(min(P, from + kPiece))));
+  if (n <= from) return;
   const int phys = a.b.table[bj];
   if (phys < 0 || phys >= a.c.n_pages) return;
-  if (vside) stage_v<D, FP4>(a.c, phys, h, n, rows);
-  else stage_k<D, FP4>(a.c, phys, h, n, rows);
+  if (vside) stage_v<D, FP4>(a.c, phys, h, from, n, rows);
+  else stage_k<D, FP4>(a.c, phys, h, from, n, rows);
   __syncthreads();
-  __bf16* dst = (vside ? a.v : a.k) + ((int64_t(b) * a.c.H + h) * a.N + int64_t(j) * P) * D;
-  for (int i = threadIdx.x; i < n * (D / 8); i += kThreads) {
+  __bf16* dst = (vside ? a.v : a.k) + ((int64_t(b) * a.c.H + h) * a.N + int64_t(j) * P + from) * D;
+  for (int i = threadIdx.x; i < (n - from) * (D / 8); i += kThreads) {
     const int r = i / (D / 8), x = i % (D / 8);
     *(cu32x4*)(dst + int64_t(i) * 8) = *(cu32x4*)(rows + r * R + x * 8);
   }
@@ -469,25 +506,14 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(ReadArgs a) {
 
 template <int D, bool FP4>
 hipError_t append(const AppendArgs& a, int64_t wgs, hipStream_t s) {
-  const int bytes = a.c.page * lds_row<D>() * 2;
-  const void* fn = (const void*)cache_append_kernel<D, FP4>;
-  if (bytes > 48 * 1024) {
-    const hipError_t e = ensure_dynamic_lds(fn, 256 * lds_row<D>() * 2);
-    if (e != hipSuccess) return e;
-  }
-  cache_append_kernel<D, FP4><<<dim3(unsigned(wgs)), kThreads, bytes, s>>>(a);
+  cache_append_kernel<D, FP4><<<dim3(unsigned(wgs)), kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
 template <int D, bool FP4>
 hipError_t read(const ReadArgs& a, hipStream_t s) {
-  const int bytes = a.c.page * lds_row<D>() * 2;
-  if (bytes > 48 * 1024) {
-    const hipError_t e = ensure_dynamic_lds((const void*)cache_read_kernel<D, FP4>, 256 * lds_row<D>() * 2);
-    if (e != hipSuccess) return e;
-  }
-  const int64_t wgs = int64_t(a.b.B) * a.b.max_pages * a.c.H * 2;
-  cache_read_kernel<D, FP4><<<dim3(unsigned(wgs)), kThreads, bytes, s>>>(a);
+  const int64_t wgs = int64_t(a.b.B) * a.b.max_pages * a.c.H * 2 * ((a.c.page + kPiece - 1) / kPiece);
+  cache_read_kernel<D, FP4><<<dim3(unsigned(wgs)), kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -509,8 +535,8 @@ hipError_t launch_cache_append(const DevCache& c, const DevBatch& b, int d, cons
   a.v_stride = v_stride;
   a.q_stride = q_stride;
   a.Hq = Hq;
-  a.page_wgs = int64_t(item_base(b.n_tokens, b.B, c.page, 2)) * c.H * 2;
-  const int64_t units = q ? int64_t(b.n_tokens) * Hq * (d / 16) : 0;
+  a.page_wgs = int64_t(item_base(b.n_tokens, b.B, c.page, 2)) * c.H * (1 + (c.page + kPiece - 1) / kPiece);
+  const int64_t units = q ? int64_t(b.n_tokens) * ((Hq + kHeads - 1) / kHeads) * (d / 16) : 0;
   const int64_t wgs = a.page_wgs + (units + kThreads - 1) / kThreads;
   if (d == 128) return c.fp4 ? append<128, true>(a, wgs, s) : append<128, false>(a, wgs, s);
   return c.fp4 ? append<64, true>(a, wgs, s) : append<64, false>(a, wgs, s);

@@ -10,7 +10,7 @@
 // running maximum, or infinity where the row does not keep the page.
 //
 // bf16 units go from memory to LDS directly, into a ring that runs three units ahead of the
-// computation (seven at d = 64): what other workgroups have not yet brought to L2 takes longer than
+// computation: what other workgroups have not yet brought to L2 takes longer than
 // two units' computation. 4-bit units run eight ahead as they lie in the page, and are widened to
 // bf16 one unit ahead, once for four waves (V's powers of two are applied there: exact).
 //
@@ -40,7 +40,7 @@ struct Stage {
   static constexpr int SIDE = 32 * D * 2;                // K or V of a unit, bf16
   static constexpr int WIDE = 2 * SIDE;
   static constexpr int PAGE = 34 * D;                    // a 4-bit unit with its scales
-  static constexpr int RING = FP4 ? 8 : D == 128 ? 4 : 8;
+  static constexpr int RING = FP4 ? 8 : 4;
   static constexpr int LOADS = FP4 ? 2 : WIDE / 1024 / kWaves;  // a wave's loads of a unit
   static constexpr int BYTES = FP4 ? 2 * WIDE + RING * PAGE : RING * WIDE;
 };

@@ -552,9 +552,10 @@ class _CacheArgs(_Args):
         self.device = None
 
     def __call__(self, t, dtype, numel, name):
+        if t is None:
+            return None
         p = super().__call__(t, dtype, numel, name)
-        if t is not None:
-            self.on(t.device, name)
+        self.on(t.device, name)
         return p
 
     def on(self, device, name):
@@ -582,11 +583,17 @@ class _CacheArgs(_Args):
         return t.data_ptr() or None, (s[0] if n > 1 else heads * d)
 
     def run(self, fn, *args):
-        self.ready()
-        if self.device is None or self.device.index == torch.cuda.current_device():
-            return fn(*args[:-1], _s(args[-1]))
-        with torch.cuda.device(self.device):
-            return fn(*args[:-1], _s(args[-1]))
+        """Small layers are bound by this host work: the raw handle of the current stream
+        costs 0.2 us, torch's stream object 5 us of a call's 13."""
+        if self.host is not None:
+            self.ready()
+        stream, index = args[-1], self.device.index
+        if index == torch._C._cuda_getDevice():
+            return fn(*args[:-1], torch._C._cuda_getCurrentRawStream(index) if stream is None
+                      else _s(stream))
+        with torch.cuda.device(index):
+            return fn(*args[:-1], torch._C._cuda_getCurrentRawStream(index) if stream is None
+                      else _s(stream))
 
 
 def _struct(cls, a, tensors, *fields):
