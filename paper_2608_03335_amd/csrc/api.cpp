@@ -906,6 +906,8 @@ spade_status spade_cache_attn(const spade_cache* c, const spade_batch* b, const 
   if (!aligned16(q) || !aligned16(o))
     return fail(SPADE_ERR_INVALID_ARG, "q and o must be 16-byte aligned");
   if (q == o) return fail(SPADE_ERR_INVALID_ARG, "q and o must not alias");
+  if (!spade::cache_attn_fits(dc, db, c->d, Hq, topk))
+    return fail(SPADE_ERR_UNSUPPORTED, "batch too large (n_tokens=%d, H=%d)", b->n_tokens, c->H);
   const size_t need = spade::cache_attn_workspace_bytes(dc, db, c->d, Hq, topk);
   if (workspace_bytes < need || (need > 0 && (workspace == nullptr || !aligned16(workspace))))
     return fail(SPADE_ERR_WORKSPACE, "16-byte aligned workspace of %zu bytes needed, %zu given", need,

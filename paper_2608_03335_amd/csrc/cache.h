@@ -73,6 +73,7 @@ struct CacheAttn {
   void* o;
   float* lse;
 };
+bool cache_attn_fits(const DevCache& c, const DevBatch& b, int d, int Hq, int topk);  // its grid
 size_t cache_attn_workspace_bytes(const DevCache& c, const DevBatch& b, int d, int Hq, int topk);
 hipError_t launch_cache_attn(const DevCache& c, const DevBatch& b, int d, const CacheAttn& p,
                              void* ws, hipStream_t s);

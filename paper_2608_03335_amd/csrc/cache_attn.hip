@@ -282,15 +282,14 @@ __device__ __forceinline__ int build_list(const AttnArgs& a, const Tile& t, uint
   if (t.nq == 1) {  // one token's list, as selections write it, is the walk already
     const int n = min(max(a.counts[row0], 0), a.topk);
     bool good = true;
-    for (int k = tid; k < n; k += kThreads) {
+    // (as many entries as the table has pages fit; a longer list cannot ascend)
+    for (int k = tid; k < min(n, a.b.max_pages); k += kThreads) {
       const int j = a.indices[row0 * a.topk + k];
       const int before = k ? a.indices[row0 * a.topk + k - 1] : -1;
       good &= j > before && j < t.pages;
       list[k] = uint32_t(j) << 16 | 1u;
     }
-    // as many entries as the table has pages fit: a longer list cannot ascend
-    if (n <= a.b.max_pages && __syncthreads_and(good)) return n;
-    __syncthreads();
+    if (__syncthreads_and(good && n <= a.b.max_pages)) return n;
   }
   for (int j = tid; j < t.pages; j += kThreads) list[j] = 0;
   __syncthreads();
@@ -567,6 +566,12 @@ hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t s) {
 }
 
 }  // namespace
+
+bool cache_attn_fits(const DevCache& c, const DevBatch& b, int d, int Hq, int topk) {
+  const Plan p = plan(c, b, d, Hq, topk);
+  const int64_t wgs = p.chunk ? chunk_items(c, b, Hq) * c.H + 8 : p.items * c.H * p.RT * p.splits;
+  return wgs <= 0x7fffffff;
+}
 
 size_t cache_attn_workspace_bytes(const DevCache& c, const DevBatch& b, int d, int Hq, int topk) {
   const Plan p = plan(c, b, d, Hq, topk);

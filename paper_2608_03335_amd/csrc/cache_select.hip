@@ -11,7 +11,7 @@
 //           into two bf16 terms. |s~ - s| <= E = 2^-13 |A|_1 M, with A = sum_g |q| and M the
 //           largest |mean| of the walk: 2^-16 A for the third term left out, G 2^-24 A for
 //           the sum over g, 2 d 2^-23 A for fp32 accumulation, each times M, and as much
-//           again to spare.
+//           again to spare; and 2^-118 (A + M + 1) for what underflows.
 //   top-k   the k-th largest s~, T, by bits of its order-preserving integer; pages above
 //           T + 2 E are in, below T - 2 E out (the k-th largest s is within E of T). Only
 //           where more pages lie between than places are left are their scores computed in
@@ -71,6 +71,25 @@ __global__ void __launch_bounds__(kThreads) cache_score_kernel(SelectArgs a) {
   if (first >= pages) return;
   const int end = min(pages, first + a.chunk_tiles * kTileP);
 
+  const int* table = a.b.table + int64_t(b) * a.b.max_pages;
+  // means of this wave's 2 x 16 pages of a tile: the A operand
+  cu32x4 f[2][KK];
+  auto load = [&](int c0) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int j = c0 + (wave * 2 + i) * 16 + (lane & 15);
+      const int phys = j < end ? table[j] : 0;
+      const bool ok = phys >= 0 && phys < a.c.n_pages;
+      const __bf16* src = (const __bf16*)a.c.mean + (int64_t(ok ? phys : 0) * a.c.H + h) * D + g * 8;
+#pragma unroll
+      for (int k = 0; k < KK; ++k) {
+        const cu32x4 x = *(const cu32x4*)(src + k * 32);
+        const cu32x4 bad = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
+        f[i][k] = ok ? x : bad;
+      }
+    }
+  };
+  load(first);  // on its way while the queries are summed
   // summed queries in two terms: the B operand
   const bool live = (lane & 15) < nq;
   const __bf16* q = a.q + (int64_t(t + (live ? lane & 15 : 0)) * a.Hq + int64_t(h) * a.G) * D + g * 8;
@@ -96,31 +115,20 @@ __global__ void __launch_bounds__(kThreads) cache_score_kernel(SelectArgs a) {
       hi[k][e] = (__bf16)sum[k][e];
       lo[k][e] = (__bf16)(sum[k][e] - float(hi[k][e]));
     }
-  const int* table = a.b.table + int64_t(b) * a.b.max_pages;
   const int64_t row = int64_t(t - a.t0 + (lane & 15)) * a.c.H + h;
   uint32_t m = 0;  // the largest |mean|, as its bits
   for (int c0 = first; c0 < end; c0 += kTileP) {
-    // means of this wave's 2 x 16 pages: the A operand
-    cu32x4 f[2][KK];
+    if (c0 > first) load(c0);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int j = c0 + (wave * 2 + i) * 16 + (lane & 15);
-      const int phys = j < end ? table[j] : 0;
-      const bool ok = phys >= 0 && phys < a.c.n_pages;
-      const __bf16* src = (const __bf16*)a.c.mean + (int64_t(ok ? phys : 0) * a.c.H + h) * D + g * 8;
+    for (int i = 0; i < 2; ++i)
+      if (c0 + (wave * 2 + i) * 16 + (lane & 15) < end)
 #pragma unroll
-      for (int k = 0; k < KK; ++k) {
-        const cu32x4 x = *(const cu32x4*)(src + k * 32);
-        const cu32x4 bad = {0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};
-        f[i][k] = ok ? x : bad;
-        if (j < end)
+        for (int k = 0; k < KK; ++k)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const uint32_t y = f[i][k][e];
             m = max(m, max(y & 0x7fff0000u, (y << 16) & 0x7fff0000u));
           }
-      }
-    }
     cf32x4 acc[2] = {};
 #pragma unroll
     for (int k = 0; k < KK; ++k)
@@ -315,6 +323,19 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : kThreads) cache_topk_kernel(S
   if (!ranked) {
     kept |= in;
   } else if (places > 0) {
+    // the summed query in fp64, 16 lanes sharing its channels. Few rows: at once, since nearly
+    // every row asks for it and waits; many rows: those that need it
+    constexpr int C = D / 16;
+    const int c0 = (lane & 15) * C;
+    double qs[C] = {};
+    auto sum_query = [&] {
+      const __bf16* q = a.q + (int64_t(t) * a.Hq + int64_t(h) * a.G) * D + c0;
+#pragma unroll 4
+      for (int i = 0; i < a.G; ++i)
+#pragma unroll
+        for (int e = 0; e < C; ++e) qs[e] += double(float(q[i * D + e]));
+    };
+    if constexpr (W > 1) sum_query();
     const float* s = a.score + (int64_t(t - a.t0) * a.c.H + h) * a.stride;
     bool odd = false;
     float top = -__builtin_huge_valf(), low = __builtin_huge_valf();
@@ -334,7 +355,8 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : kThreads) cache_topk_kernel(S
     for (int i = lane; i * a.chunk_tiles * kTileP < vis; i += 64) big = max(big, __float_as_uint(m[i]));
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) big = max(big, __shfl_xor(big, o));
-    const float E = a.a1[(int64_t(t - a.t0)) * a.c.H + h] * __uint_as_float(big) * 0x1p-13f;
+    const float A = a.a1[int64_t(t - a.t0) * a.c.H + h], M = __uint_as_float(big);
+    const float E = A * M * 0x1p-13f + (A + M + 1.0f) * 0x1p-118f;
     odd |= !(E <= 1.0e37f);
     const bool exact_all = team.sum(__popcll(__ballot(odd))) > 0;
     uint32_t open = in;  // pages to rank in fp64
@@ -364,15 +386,7 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : kThreads) cache_topk_kernel(S
       }
     }
     if (need > 0) {
-      // fp64 scores, four pages at a time: 16 lanes share a page's channels
-      constexpr int C = D / 16;
-      const int c0 = (lane & 15) * C;
-      double qs[C] = {};
-      const __bf16* q = a.q + (int64_t(t) * a.Hq + int64_t(h) * a.G) * D + c0;
-#pragma unroll 4
-      for (int i = 0; i < a.G; ++i)
-#pragma unroll
-        for (int e = 0; e < C; ++e) qs[e] += double(float(q[i * D + e]));
+      if constexpr (W == 1) sum_query();
       // key of the page this lane's 16 lanes were given (-1: none)
       auto page_key = [&](int page) {
         double x = 0.0;
@@ -548,7 +562,7 @@ Plan plan(const DevCache& c, const DevBatch& b) {
   // a workgroup walks several page tiles (its start costs as much as five) where the card is
   // full without more of them
   const int64_t items = int64_t(item_base(p.tokens, b.B, kTileQ, 1)) * c.H;
-  const int64_t want = (512 + items - 1) / items;
+  const int64_t want = (1024 + items - 1) / items;
   p.chunk_tiles = int(want >= tiles ? 1 : (tiles + want - 1) / want);
   p.chunks = (tiles + p.chunk_tiles - 1) / p.chunk_tiles;
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };

@@ -191,3 +191,65 @@ def test_raster_attention_from_the_cache():
     other = out[0].transpose(0, 1).cpu().double()
     # the block attention also rounds the weights it sums to bf16: 2^-8 of the value more
     assert bool(((other - want).abs() <= tol + C.BF16_HALF * want.abs()).all())
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+def test_a_batch_of_many_sequences(fp4):
+    """1500 sequences, more than a workgroup has threads, of 0 to 70 tokens with 0 to 2 new ones:
+    append in place (q_out is q), select and attend."""
+    B, Hq, H, d, P = 1500, 4, 2, 64, 32
+    lens = [(b * 37) % 71 for b in range(B)]
+    news = [min(b % 3, L) for b, L in enumerate(lens)]
+    x = C.Batch(lens, news, Hq, H, d, P, fp4, seed=9, held=[L - n for L, n in zip(lens, news)])
+    x.to_device()
+    q = x.q.to(DEV).clone()
+    cos, sin = grid_rope(2, 6, 6, d, device="cpu")
+    S.spade_cache_append(x.c, x.b, x.new(x.k).to(DEV), x.new(x.v).to(DEV), q, q,
+                         S.rope(cos.to(DEV), sin.to(DEV)))
+    counts = torch.zeros(x.n, H, dtype=torch.int32, device=DEV)
+    idx = torch.full((x.n, H, 2), -1, dtype=torch.int32, device=DEV)
+    ws = x.workspace(2)
+    S.spade_cache_select(x.c, x.b, q, 2, counts, idx, workspace=ws)
+    o = torch.empty(x.n, Hq, d, dtype=torch.bfloat16, device=DEV)
+    lse = torch.empty(x.n, Hq, dtype=torch.float32, device=DEV)
+    S.spade_cache_attn(x.c, x.b, q, 0.125, o, lse, counts, idx, workspace=ws)
+    torch.cuda.synchronize()
+    place = torch.cat([torch.arange(L - n, L) for L, n in zip(lens, news)])
+    qr = C.rotate(x.q, cos[place], sin[place], False)
+    assert torch.equal(q.cpu().view(torch.int16), qr.view(torch.int16))
+    keys = [torch.cat([C.stored(k[:L - n], fp4), C.stored(C.rotate(k[L - n:], cos[L - n:L], sin[L - n:L], False), fp4)])
+            for k, L, n in zip(x.k, lens, news)]
+    rows = x.rows()
+    picked = [r for r in rows if r[2] and r[0] % 25 < 3] + [rows[-1]]
+    for b, t0, n in picked:
+        seen = C.seen_by(lens[b], n, True)
+        lists = C.select(qr[t0:t0 + n], C.page_means(keys[b], P), seen, P, 2, 0, 1)
+        got = [idx[t0 + i // H, i % H, :len(r)].tolist() for i, r in enumerate(lists)]
+        assert counts[t0:t0 + n].flatten().tolist() == [len(r) for r in lists] and got == lists, b
+        ro, rl, ot, lt = C.attend(qr[t0:t0 + n], keys[b], C.stored(x.v[b], fp4), seen, lists, P, 0.125)
+        assert bool(((o[t0:t0 + n].cpu().double() - ro).abs() <= ot).all()), b
+        assert bool(((lse[t0:t0 + n].cpu().double() - rl).abs() <= lt).all()), b
+
+
+def test_captured_prompt_chunk():
+    """A chunk of many tokens (the kernel of shared tiles) and its selection under capture."""
+    B, Hq, H, d = 1, 64, 64, 64
+    p = CachePath(B, Hq, H, d, n_pages=30, max_pages=20, max_tokens=300, page=32, topk=3, sink=1,
+                  local=1, device=DEV)
+    gen = torch.Generator().manual_seed(5)
+    rand = lambda h: torch.randn(300, h, d, generator=gen).to(torch.bfloat16).to(DEV)  # noqa: E731
+    q, k, v = rand(Hq), rand(H), rand(H)
+    p.plan([300])
+    want = p.run(q, k, v).clone()
+    torch.cuda.synchronize()
+    o = torch.empty_like(want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        p.run(q, k, v, out=o)
+    for _ in range(3):
+        o.fill_(float("nan"))
+        p.workspace.fill_(77)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, want)
+        _ = (q.float() * 2).sum().item()

@@ -146,3 +146,41 @@ def test_the_longest_table():
         n = min(topk, 16384)
         assert int(counts) == n
         assert torch.equal(idx[0, 0, :n].cpu().long(), torch.sort(order[:n])[0])
+
+
+@pytest.mark.parametrize("size", [1e-38, 1e-30, 1e30, 2e37])
+def test_very_small_and_very_large_scores(size):
+    """Sizes at which fp32 scores underflow or overflow: fp64 still ranks."""
+    P, d, pages = 32, 64, 80
+    x = C.Batch([P * pages], [2], 4, 2, d, P, False, seed=6)
+    x.q = (x.q.double() * size).to(torch.bfloat16)
+    x.hold([P * pages])
+    x.to_device()
+    assert _run(x, x.q, 20, 1, 2, True) == x.ref_select(x.q, True, 20, 1, 2)
+
+
+@pytest.mark.parametrize("pages", [255, 257, 1023, 1025, 4095, 4097])
+def test_page_counts_at_the_edges_of_the_row_kernels(pages):
+    """One wave, four and sixteen a row; few rows and many; more kept than 64 pages in doubt."""
+    P, d = 32, 64
+    gen = torch.Generator().manual_seed(pages)
+    mean = torch.randn(pages, 2, d, generator=gen).to(torch.bfloat16)
+    mean[10:100] = mean[10]                       # ninety pages alike
+    kv = torch.empty(pages, 2, P, d, dtype=torch.bfloat16, device=DEV)
+    c = S.cache(S.SPADE_CACHE_BF16, 2, d, P, kv, kv, mean.to(DEV))
+    table = torch.arange(pages, dtype=torch.int32, device=DEV)[None]
+    for n in (3, 1100):
+        q = torch.randn(n, 2, d, generator=gen).to(torch.bfloat16)
+        q[0, 0] = mean[10, 0]                     # the alike pages lead this row
+        b = S.batch(table, torch.tensor([P * pages - 5], dtype=torch.int32, device=DEV),
+                    torch.tensor([0, n], dtype=torch.int32, device=DEV), n)
+        for topk in (40, 150):
+            counts = torch.zeros(n, 2, dtype=torch.int32, device=DEV)
+            idx = torch.full((n, 2, topk), -1, dtype=torch.int32, device=DEV)
+            ws = torch.empty(S.spade_cache_select_workspace_bytes(c, b, 2, topk), dtype=torch.uint8, device=DEV)
+            S.spade_cache_select(c, b, q.to(DEV), topk, counts, idx, causal=False, local=1, workspace=ws)
+            score = torch.einsum("nhc,jhc->nhj", q.double(), mean.double())
+            score[..., pages - 1] = float("inf")
+            order = torch.sort(score, dim=-1, stable=True, descending=True)[1][..., :topk]
+            assert bool((counts == min(topk, pages)).all())
+            assert torch.equal(idx[..., :min(topk, pages)].cpu().long(), torch.sort(order, -1)[0]), (n, topk)
