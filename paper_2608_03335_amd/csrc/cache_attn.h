@@ -30,9 +30,10 @@ struct AttnArgs {
   int wgs;                  // workgroups a call is split into, about
 };
 
-// Many queries a sequence: tiles of 128 rows that share staged keys (cache_chunk.hip).
-// chunk_items: work items, 0 where the kernel does not serve the call.
-int64_t chunk_items(const DevCache& c, const DevBatch& b, int Hq);
+// Many queries a sequence: tiles of 128 rows, four waves of 32, that share staged keys
+// (cache_chunk.hip). A wave holds kChunkRows / G tokens.
+constexpr int kChunkRows = 32, kChunkWaves = 4;
+constexpr int kChunkUnits = 32;  // units of 32 keys a split of such a tile is worth, at least
 hipError_t launch_chunk_attn(const AttnArgs& a, int d, hipStream_t s);
 
 #ifdef __HIPCC__

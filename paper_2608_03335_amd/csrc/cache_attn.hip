@@ -29,12 +29,13 @@ namespace {
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kMaxSplits = 64;
+constexpr int kCUs = 256;
 constexpr int kMinUnits = 16;      // units a split is worth: its start and join cost as much
 // Workgroups that are on the card at once (256 CUs, by registers): a call is split into about
 // as many. On 64 4-bit contexts of up to 16384 tokens: 384 186 us, 512 183, 768 175, 1024 177,
 // 2048 200; two of 131072 in bf16: 384 108, 512 106, 768 and more 117.
 template <int D, bool FP4>
-constexpr int target_wgs() { return 256 * (D == 128 && !FP4 ? 2 : 3); }
+constexpr int target_wgs() { return kCUs * (D == 128 && !FP4 ? 2 : 3); }
 constexpr float kLazy = 8.0f;      // the running maximum is raised when a row's grew by 2^8
 
 // What a work item covers.
@@ -474,22 +475,24 @@ __global__ void __launch_bounds__(kThreads, FP4 ? 3 : 2) cache_attn_kernel(AttnA
   }
 }
 
-// Joins the splits of one tile, in split order: a wave takes one row.
-template <int D>
+// Joins the splits of one tile of ROWS rows, in split order: a wave takes one row. Rows lie in
+// groups of GROUP (a wave's), a group's tokens one after the other with their heads.
+template <int D, int ROWS, int GROUP>
 __global__ void __launch_bounds__(kThreads) cache_join_kernel(AttnArgs a) {
   constexpr int PIECES = D / 4, RUNS = 64 / PIECES;
-  constexpr int64_t STRIDE = 16 * D + 32;
+  constexpr int64_t STRIDE = ROWS * (D + 2);
   const JoinHead t = a.join[blockIdx.x];
   if (t.splits <= 1) return;
   const int lane = threadIdx.x & 63, c4 = lane % PIECES, run = lane / PIECES;
   const int row = blockIdx.y * kWaves + (threadIdx.x >> 6);
-  const int rq = row / t.heads, gh = row - rq * t.heads;
-  if (rq >= t.nq) return;
+  const int in_group = row % GROUP, q = in_group / t.heads, gh = in_group - q * t.heads;
+  const int per_group = GROUP / t.heads, rq = row / GROUP * per_group + q;
+  if (q >= per_group || rq >= t.nq) return;
   const float* po = a.part + int64_t(blockIdx.x) * a.splits * STRIDE;
   static_assert(kMaxSplits <= 64, "a lane holds one split's statistics");
   const bool in = lane < t.splits;
-  const float m = in ? po[lane * STRIDE + 16 * D + row * 2] : kNegInf;
-  const float l = in ? po[lane * STRIDE + 16 * D + row * 2 + 1] : 0.0f;
+  const float m = in ? po[lane * STRIDE + ROWS * D + row * 2] : kNegInf;
+  const float l = in ? po[lane * STRIDE + ROWS * D + row * 2 + 1] : 0.0f;
   float top = m;
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
@@ -519,30 +522,54 @@ struct Plan {
   int lds;
 };
 
+// Splits for a launch of `wgs` workgroups that should be about `want`, of walks of `pages`.
+int splits_of(int64_t want, int64_t wgs, int64_t pages, int page, int least_units) {
+  const int64_t most = (pages * (page / 32) + least_units - 1) / least_units;
+  int64_t s = want / (wgs < 1 ? 1 : wgs);
+  s = s < most ? s : most;
+  s = s < kMaxSplits ? s : kMaxSplits;
+  return int(s < 1 ? 1 : s);
+}
+
 Plan plan(const DevCache& c, const DevBatch& b, int d, int Hq, int topk) {
   Plan p;
   p.G = Hq / c.H;
+  p.wgs = d == 128 ? (c.fp4 ? target_wgs<128, true>() : target_wgs<128, false>())
+                   : (c.fp4 ? target_wgs<64, true>() : target_wgs<64, false>());
+  const int64_t each = (int64_t(b.n_tokens) + b.B - 1) / b.B;  // tokens a sequence, on average
+  const int64_t holders = b.B < b.n_tokens ? b.B : b.n_tokens;  // sequences with tokens, at most
+  auto walk = [&](int64_t tokens) {                             // pages a tile walks, at most
+    return topk && topk * tokens < b.max_pages ? topk * tokens : int64_t(b.max_pages);
+  };
+  // Many rows a sequence: tiles of 128 rows share their keys, where they fill half the card. Calls
+  // that read all tokens split the keys of such tiles to fill it twice. Measured, in us, this side
+  // and tiles of 16 rows (bf16, width 128, one sequence; Hq x H, context, new tokens):
+  //   all tokens   16 x 4, 8192, 500: 61, 102    32 x 8, 16384, 200: 90, 154   64: 53, 55   24: 39, 37
+  //                12 x 12, 16384, 1200: 175, 323, and 398 without splits; 32 x 8, 4-bit, 200: 112, 165
+  //   listed pages 32 x 8, 16384, 200, 32 pages: 78, 62    16 x 4, width 64, 4-bit, 400, 24: 49, 36
+  // Lists leave a tile's rows little in common, so what fills the card is more and smaller tiles.
+  const int64_t rows = int64_t(b.n_tokens) * p.G;
+  p.chunk = false;
+  if (p.G <= kChunkRows && rows >= int64_t(b.B) * 64) {
+    p.QT = kChunkRows / p.G * kChunkWaves;
+    p.RT = 1;
+    p.items = item_base(b.n_tokens, b.B, p.QT, 1);
+    p.lds = 0;
+    p.splits = 1;
+    if (!topk && rows >= int64_t(b.B) * 128) {
+      const int64_t wgs = (b.n_tokens / p.QT + holders) * c.H;
+      p.splits = splits_of(2 * kCUs, wgs, b.max_pages, c.page, kChunkUnits);
+      p.chunk = wgs * p.splits >= kCUs / 2;
+    }
+    p.chunk = p.chunk || rows / 128 * c.H >= kCUs / 2;
+    if (p.chunk) return p;
+  }
   p.QT = p.G < 16 ? 16 / p.G : 1;
   p.RT = (p.G + 15) / 16;
   p.items = p.QT > 1 ? item_base(b.n_tokens, b.B, p.QT, 1) : b.n_tokens;
-  p.splits = 1;
-  p.wgs = d == 128 ? (c.fp4 ? target_wgs<128, true>() : target_wgs<128, false>())
-                   : (c.fp4 ? target_wgs<64, true>() : target_wgs<64, false>());
-  // many rows a sequence: tiles of 128 rows share their keys, where they fill the card
-  const int64_t rows = int64_t(b.n_tokens) * p.G;
-  p.chunk = p.G <= 32 && rows >= int64_t(b.B) * 64 && rows / 128 * c.H >= 128;
-  if (p.chunk) return p;
   // workgroups without splits: tiles that hold tokens (at most), heads, row tiles
-  const int64_t tiles = p.QT > 1 ? b.n_tokens / p.QT + (b.B < b.n_tokens ? b.B : b.n_tokens) : b.n_tokens;
-  const int64_t wgs = tiles * c.H * p.RT;
-  int64_t walk = b.max_pages;
-  const int64_t each = (int64_t(b.n_tokens) + b.B - 1) / b.B;  // tokens a sequence, on average
-  if (topk && topk * (each < p.QT ? each : p.QT) < walk) walk = topk * (each < p.QT ? each : p.QT);
-  int64_t s = (2 * p.wgs + wgs - 1) / wgs;
-  const int64_t most = (walk * (c.page / 32) + kMinUnits - 1) / kMinUnits;
-  s = s < most ? s : most;
-  s = s < kMaxSplits ? s : kMaxSplits;
-  p.splits = int(s < 1 ? 1 : s);
+  const int64_t wgs = (p.QT > 1 ? b.n_tokens / p.QT + holders : b.n_tokens) * c.H * p.RT;
+  p.splits = splits_of(2 * p.wgs + wgs - 1, wgs, walk(each < p.QT ? each : p.QT), c.page, kMinUnits);
   p.lds = kWaves * 16 * (d + 4) * 4 + (topk ? (b.max_pages * 4 + 15) / 16 * 16 : 0);
   return p;
 }
@@ -558,10 +585,19 @@ hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t s) {
   }
   const int64_t tiles = p.items * a.c.H * p.RT;
   cache_attn_kernel<D, FP4><<<dim3(unsigned(tiles * p.splits)), kThreads, p.lds, s>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.splits == 1) return e;
-  const int rows = p.QT * (p.G < 16 ? p.G : 16);
-  cache_join_kernel<D><<<dim3(unsigned(tiles), (rows + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t join(const AttnArgs& a, const Plan& p, hipStream_t s) {
+  const unsigned tiles = unsigned(p.items * a.c.H * p.RT);
+  if (p.chunk) {
+    cache_join_kernel<D, kChunkRows * kChunkWaves, kChunkRows>
+        <<<dim3(tiles, kChunkRows * kChunkWaves / kWaves), kThreads, 0, s>>>(a);
+  } else {
+    const int rows = p.QT * (p.G < 16 ? p.G : 16);
+    cache_join_kernel<D, 16, 16><<<dim3(tiles, (rows + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
+  }
   return hipGetLastError();
 }
 
@@ -569,15 +605,14 @@ hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t s) {
 
 bool cache_attn_fits(const DevCache& c, const DevBatch& b, int d, int Hq, int topk) {
   const Plan p = plan(c, b, d, Hq, topk);
-  const int64_t wgs = p.chunk ? chunk_items(c, b, Hq) * c.H + 8 : p.items * c.H * p.RT * p.splits;
-  return wgs <= 0x7fffffff;
+  return p.items * c.H * p.RT * p.splits + 8 <= 0x7fffffff;
 }
 
 size_t cache_attn_workspace_bytes(const DevCache& c, const DevBatch& b, int d, int Hq, int topk) {
   const Plan p = plan(c, b, d, Hq, topk);
-  if (p.chunk || p.splits == 1) return 0;
-  const size_t tiles = size_t(p.items) * c.H * p.RT;
-  return join_bytes(tiles) + tiles * p.splits * (16 * d + 32) * 4;
+  if (p.splits == 1) return 0;
+  const size_t tiles = size_t(p.items) * c.H * p.RT, rows = p.chunk ? kChunkRows * kChunkWaves : 16;
+  return join_bytes(tiles) + tiles * p.splits * rows * (d + 2) * 4;
 }
 
 hipError_t launch_cache_attn(const DevCache& c, const DevBatch& b, int d, const CacheAttn& x,
@@ -603,9 +638,12 @@ hipError_t launch_cache_attn(const DevCache& c, const DevBatch& b, int d, const 
   a.splits = p.splits;
   a.items = p.items;
   a.wgs = p.wgs;
-  if (p.chunk) return launch_chunk_attn(a, d, s);
-  if (d == 128) return c.fp4 ? run<128, true>(a, p, s) : run<128, false>(a, p, s);
-  return c.fp4 ? run<64, true>(a, p, s) : run<64, false>(a, p, s);
+  hipError_t e;
+  if (p.chunk) e = launch_chunk_attn(a, d, s);
+  else if (d == 128) e = c.fp4 ? run<128, true>(a, p, s) : run<128, false>(a, p, s);
+  else e = c.fp4 ? run<64, true>(a, p, s) : run<64, false>(a, p, s);
+  if (e != hipSuccess || p.splits == 1) return e;
+  return d == 128 ? join<128>(a, p, s) : join<64>(a, p, s);
 }
 
 }  // namespace spade

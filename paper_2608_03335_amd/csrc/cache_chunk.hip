@@ -27,9 +27,9 @@ namespace {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) char lds_char;
 
-constexpr int kWaves = 4;
+constexpr int kWaves = kChunkWaves;
 constexpr int kThreads = 64 * kWaves;
-constexpr int kRows = 32;          // rows of a wave
+constexpr int kTileRows = kChunkRows * kWaves;
 constexpr int kSeg = 512;          // pages walked before the masks are built anew
 constexpr float kLazy = 8.0f;
 
@@ -192,24 +192,35 @@ __device__ __forceinline__ void step(const char* kf, const char* vf, Rows<D>& w,
 }
 
 template <int D, bool FP4>
-__global__ void __launch_bounds__(kThreads, 2) cache_chunk_kernel(AttnArgs a, int64_t items) {
+__global__ void __launch_bounds__(kThreads, 2) cache_chunk_kernel(AttnArgs a) {
   using ST = Stage<D, FP4>;
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ Seg sg;
-  // each XCD takes a run of neighbouring items of a head: they want the same pages
-  const int64_t total = items * a.c.H, per = (total + 7) >> 3;
+  // each XCD takes a run of neighbouring items of a head and split: they want the same pages
+  const int64_t items = a.items, total = items * a.c.H * a.splits, per = (total + 7) >> 3;
   const int64_t slot = blockIdx.x >> 3, L = (blockIdx.x & 7) * per + slot;
   if (slot >= per || L >= total) return;
-  const int h = int(L / items);
-  const SeqItem it = find_item(a.b, int(L - h * items), a.QT, 1);
-  if (it.b < 0) return;
+  const int hs = int(L / items), item = int(L - hs * items), h = hs / a.splits, split = hs - h * a.splits;
+  JoinHead* head = a.join + int64_t(item) * a.c.H + h;
+  const SeqItem it = find_item(a.b, item, a.QT, 1);
   const int skip = it.first * a.QT;
-  if (skip >= it.n) return;
+  if (it.b < 0 || skip >= it.n) {
+    if (a.splits > 1 && split == 0 && threadIdx.x == 0) *head = JoinHead{0, 0, 0, 0, 0};
+    return;
+  }
   const int t0 = it.t0 + skip, nq = min(a.QT, it.n - skip);
   Seen seen = seen_of(a, it);
   seen.first += skip * seen.step;
   const int P = a.c.page, upp = P >> 5;
-  const int pages = (seen.of(nq - 1) + P - 1) / P;
+  const int visible = (seen.of(nq - 1) + P - 1) / P;
+  // splits share the pages of a long tile evenly
+  int splits = 1;
+  if (a.splits > 1) {
+    splits = min(max((visible * upp + kChunkUnits - 1) / kChunkUnits, 1), a.splits);
+    if (split == 0 && threadIdx.x == 0) *head = JoinHead{splits, t0, nq, h * a.G, a.G};
+    if (split >= splits) return;
+  }
+  const int page0 = int(int64_t(visible) * split / splits), pages = int(int64_t(visible) * (split + 1) / splits);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
@@ -241,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 2) cache_chunk_kernel(AttnArgs a, in
     w.l = 0.0f;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) w.o[c] = f32x16{};
-    for (int seg0 = 0; seg0 < pages; seg0 += kSeg) {
+    for (int seg0 = page0; seg0 < pages; seg0 += kSeg) {
       const int span = min(kSeg, pages - seg0);
       __syncthreads();  // the last segment's masks are no longer read
       if (a.topk) {
@@ -376,7 +387,17 @@ __global__ void __launch_bounds__(kThreads, 2) cache_chunk_kernel(AttnArgs a, in
     }
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(w.l), __float_as_uint(w.l), false, false);
     const float l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    if (live && (only < 0 || qi == only)) {
+    if (live && (only < 0 || qi == only) && splits > 1) {
+      const int row = wave * kChunkRows + r;
+      float* po = a.part + ((int64_t(item) * a.c.H + h) * a.splits + split) * (kTileRows * (D + 2));
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *(cf32x4*)(po + row * D + c * 32 + 2 * i + 4 * half) =
+              cf32x4{w.o[c][i], w.o[c][i + 1], w.o[c][i + 2], w.o[c][i + 3]};
+      if (half == 0) *(cf32x2*)(po + kTileRows * D + row * 2) = cf32x2{w.m, l};
+    } else if (live && (only < 0 || qi == only)) {
       const float inv = w.m == kNegInf ? 0.0f : 1.0f / l;
 #pragma unroll
       for (int c = 0; c < D / 32; ++c)
@@ -394,31 +415,22 @@ __global__ void __launch_bounds__(kThreads, 2) cache_chunk_kernel(AttnArgs a, in
 }
 
 template <int D, bool FP4>
-hipError_t run(const AttnArgs& a, int64_t items, hipStream_t s) {
+hipError_t run(const AttnArgs& a, hipStream_t s) {
   const int bytes = Stage<D, FP4>::BYTES;
   if (bytes > 32 * 1024) {
     const hipError_t e = ensure_dynamic_lds((const void*)cache_chunk_kernel<D, FP4>, bytes);
     if (e != hipSuccess) return e;
   }
-  const int64_t wgs = (items * a.c.H + 7) / 8 * 8;
-  cache_chunk_kernel<D, FP4><<<dim3(unsigned(wgs)), kThreads, bytes, s>>>(a, items);
+  const int64_t wgs = (a.items * a.c.H * a.splits + 7) / 8 * 8;
+  cache_chunk_kernel<D, FP4><<<dim3(unsigned(wgs)), kThreads, bytes, s>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t chunk_items(const DevCache& c, const DevBatch& b, int Hq) {
-  const int G = Hq / c.H;
-  if (G > kRows) return 0;
-  return item_base(b.n_tokens, b.B, kRows / G * kWaves, 1);
-}
-
-hipError_t launch_chunk_attn(const AttnArgs& x, int d, hipStream_t s) {
-  AttnArgs a = x;
-  a.QT = kRows / a.G * kWaves;
-  const int64_t items = chunk_items(a.c, a.b, a.Hq);
-  if (d == 128) return a.c.fp4 ? run<128, true>(a, items, s) : run<128, false>(a, items, s);
-  return a.c.fp4 ? run<64, true>(a, items, s) : run<64, false>(a, items, s);
+hipError_t launch_chunk_attn(const AttnArgs& a, int d, hipStream_t s) {
+  if (d == 128) return a.c.fp4 ? run<128, true>(a, s) : run<128, false>(a, s);
+  return a.c.fp4 ? run<64, true>(a, s) : run<64, false>(a, s);
 }
 
 }  // namespace spade
