@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(kThreads, FP4 ? 3 : 2) cache_attn_kernel(AttnA
 // groups of GROUP (a wave's), a group's tokens one after the other with their heads.
 template <int D, int ROWS, int GROUP>
 __global__ void __launch_bounds__(kThreads) cache_join_kernel(AttnArgs a) {
-  constexpr int PIECES = D / 4, RUNS = 64 / PIECES;
+  constexpr int PIECES = D / 4, RUNS = 64 / PIECES, AHEAD = 8;
   constexpr int64_t STRIDE = ROWS * (D + 2);
   const JoinHead t = a.join[blockIdx.x];
   if (t.splits <= 1) return;
@@ -489,6 +489,15 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(AttnArgs a) {
   const int per_group = GROUP / t.heads, rq = row / GROUP * per_group + q;
   if (q >= per_group || rq >= t.nq) return;
   const float* po = a.part + int64_t(blockIdx.x) * a.splits * STRIDE;
+  // loads of the partial results a batch ahead of their use, the first ahead of the statistics
+  cf32x4 next[AHEAD];
+  auto fetch = [&](int s0) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      next[i] = *(const cf32x4*)(po + min(s0 + i * RUNS + run, t.splits - 1) * STRIDE + row * D + c4 * 4);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  fetch(0);
   static_assert(kMaxSplits <= 64, "a lane holds one split's statistics");
   const bool in = lane < t.splits;
   const float m = in ? po[lane * STRIDE + ROWS * D + row * 2] : kNegInf;
@@ -501,12 +510,17 @@ __global__ void __launch_bounds__(kThreads) cache_join_kernel(AttnArgs a) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
   cf32x4 x{};
-#pragma unroll 8
-  for (int s0 = 0; s0 < t.splits; s0 += RUNS) {
-    const int s = min(s0 + run, t.splits - 1);
-    const float fs = __shfl(f, s);
-    const cf32x4 y = *(const cf32x4*)(po + s * STRIDE + row * D + c4 * 4);
-    if (s0 + run < t.splits) x += y * fs;
+  for (int s0 = 0; s0 < t.splits; s0 += AHEAD * RUNS) {
+    cf32x4 y[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) y[i] = next[i];
+    if (s0 + AHEAD * RUNS < t.splits) fetch(s0 + AHEAD * RUNS);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int s = s0 + i * RUNS + run;
+      const float fs = __shfl(f, min(s, t.splits - 1));
+      if (s < t.splits) x += y[i] * fs;
+    }
   }
 #pragma unroll
   for (int o = PIECES; o < 64; o <<= 1)
