@@ -17,6 +17,12 @@
 // that no element is off by more than half a step of its place in {0,.5,1,1.5,2,3,4,6} 2^e
 // (7 is half way between 6 and the next step, 8); nearest, ties to even. At e = 126 the
 // grid ends at 3 2^126, the last value bf16 can hold.
+//
+// Bound by HBM for many tokens, by the launch for few. Pieces of 64 tokens keep four
+// workgroups a CU under way (whole pages of 128: 143 us where they take 126). Measured: 4680
+// new tokens of 12 heads of 128, bf16, 89 MB with the queries 18.6 us (4.8 TB/s); 27673 tokens
+// of 32 query and 8 K/V heads in 4 bits, 597 MB, 126 us (4.7 TB/s); one token of 32 sequences
+// 7.7 us.
 #include "cache.h"
 
 namespace spade {
@@ -156,9 +162,9 @@ __device__ __forceinline__ int64_t page_elem(const DevCache& c, int phys, int h)
   return (int64_t(phys) * c.H + h) * c.page * D;
 }
 
-// Tokens [from, n) of a page's K side as rows in LDS, the first at `rows` (from a multiple of
-// 32, n <= page; whole tiles are read).
-template <int D, bool FP4>
+// Tokens [from, n) of a page's K side, a piece at most, as rows in LDS, the first at `rows` (from
+// a multiple of 32, n <= page; whole tiles are read), LOADS 16-byte loads at a time in bf16.
+template <int D, bool FP4, int LOADS>
 __device__ __forceinline__ void stage_k(const DevCache& c, int phys, int h, int from, int n, __bf16* rows) {
   constexpr int R = lds_row<D>();
   const int tiles = (n + 15) >> 4, tile0 = from >> 4;
@@ -166,57 +172,83 @@ __device__ __forceinline__ void stage_k(const DevCache& c, int phys, int h, int 
   const int64_t base = page_elem<D>(c, phys, h);
   if constexpr (!FP4) {
     const cu32x4* src = (const cu32x4*)((const __bf16*)c.k + base);
-    for (int i = tile0 * 2 * D + threadIdx.x; i < tiles * 2 * D; i += kThreads) {
-      const int m = i & 15, sg = (i >> 4) % (D / 8), tile = i / (2 * D);
-      const int r = tile * 16 + m;
-      if (r < n) *(cu32x4*)(rows + r * R + sg * 8) = src[i];
+    for (int i0 = tile0 * 2 * D + threadIdx.x; i0 < tiles * 2 * D; i0 += LOADS * kThreads) {
+      cu32x4 x[LOADS];
+#pragma unroll
+      for (int t = 0; t < LOADS; ++t)
+        if (i0 + t * kThreads < tiles * 2 * D) x[t] = src[i0 + t * kThreads];
+#pragma unroll
+      for (int t = 0; t < LOADS; ++t) {
+        const int i = i0 + t * kThreads, m = i & 15, sg = (i >> 4) % (D / 8), r = i / (2 * D) * 16 + m;
+        if (r < n) *(cu32x4*)(rows + r * R + sg * 8) = x[t];
+      }
     }
-  } else {
-    const uint8_t* src = (const uint8_t*)c.k + base / 2;
-    const uint8_t* sc = c.ks + base / 32;
-    for (int i = tile0 * 2 * D + threadIdx.x; i < tiles * 2 * D; i += kThreads) {
-      // one dword: 8 channels of token (tile, m), lane group g
-      const int w = i % (D / 32), gm = i / (D / 32) % 64, tile = i / (2 * D);
-      const int g = gm >> 4, m = gm & 15, r = tile * 16 + m;
-      const int ch = g * (D / 4) + w * 8;
-      const uint32_t x = *(const uint32_t*)(src + int64_t(i) * 4);
-      const float s = scale_of(sc[tile * (D / 2) + (ch >> 5) * 16 + m]);
-      if (r < n) *(cbf16x8*)(rows + r * R + ch) = fp4_eight(x, s);
+  } else {  // a thread: the D / 4 channels of lane group g of a token
+    static_assert(kPiece / 16 * 64 == kThreads, "a thread a token and lane group");
+    constexpr int W = D / 32;
+    typedef uint32_t words __attribute__((ext_vector_type(W)));
+    const int tile = tile0 + int(threadIdx.x >> 6), g = (threadIdx.x >> 4) & 3, m = threadIdx.x & 15;
+    const int r = tile * 16 + m, ch = g * (D / 4);
+    if (r < n) {
+      const words x = ((const words*)((const uint8_t*)c.k + base / 2))[tile * 64 + (threadIdx.x & 63)];
+      const float s = scale_of(c.ks[base / 32 + tile * (D / 2) + (ch >> 5) * 16 + m]);
+#pragma unroll
+      for (int w = 0; w < W; ++w) *(cbf16x8*)(rows + r * R + ch + w * 8) = fp4_eight(x[w], s);
     }
   }
 }
 
-// The same for the V side.
+// The same for the V side: a thread turns two neighbouring channels of eight tokens at a time.
 template <int D, bool FP4>
 __device__ __forceinline__ void stage_v(const DevCache& c, int phys, int h, int from, int n, __bf16* rows) {
-  constexpr int R = lds_row<D>();
+  constexpr int R = lds_row<D>(), N = kPiece / 32 * 2 * D / kThreads;
   const int blocks = (n + 31) >> 5, block0 = from >> 5;
   rows -= from * R;
   const int64_t base = page_elem<D>(c, phys, h);
-  for (int i = block0 * 4 * D + threadIdx.x; i < blocks * 4 * D; i += kThreads) {
-    const int kb = i / (4 * D);
-    cbf16x8 x;
-    int ch, g;
-    if constexpr (!FP4) {  // i = (kb, ct, g, m)
-      const int m = i & 15, ct = (i >> 6) % (D / 16);
-      g = (i >> 4) & 3;
-      ch = ct * 16 + m;
-      x = *(const cbf16x8*)((const __bf16*)c.v + base + int64_t(i) * 8);
-    } else {  // i = (kb, half, g, m, ct)
-      const int ct = i & 3, m = (i >> 2) & 15, half = (i >> 8) % (D / 64);
-      g = (i >> 6) & 3;
-      ch = (half * 4 + ct) * 16 + m;
-      const uint32_t w = *(const uint32_t*)((const uint8_t*)c.v + base / 2 + int64_t(i) * 4);
-      const uint8_t* sc = c.vs + base / 32 + kb * D + (g * (D / 32) + (ch >> 5)) * 8;
-      const cbf16x8 y = fp4_eight(w, 1.0f);
-      // a power of two times an e2m1 value: exact in bf16
+  cbf16x8 x[N][2];
+  uint32_t w[N][2];
+  cu32x2 sc[N];
+  int kb[N], ch[N], g[N];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = (__bf16)(float(y[j]) * scale_of(sc[j]));
+  for (int t = 0; t < N; ++t) {
+    const int p = t * kThreads + int(threadIdx.x), y = p % (2 * D);
+    kb[t] = block0 + p / (2 * D);
+    if constexpr (!FP4) {  // units (ct, g, m) of a block
+      g[t] = (y >> 3) & 3;
+      ch[t] = (y >> 5) * 16 + (y & 7) * 2;
+      const cbf16x8* src = (const cbf16x8*)((const __bf16*)c.v + base) + kb[t] * 4 * D + 2 * y;
+      if (kb[t] < blocks) x[t][0] = src[0], x[t][1] = src[1];
+    } else {  // (half, g, m, ct)
+      const int ct = y & 3, m = ((y >> 2) & 7) * 2, half = y >> 7;
+      g[t] = (y >> 5) & 3;
+      ch[t] = (half * 4 + ct) * 16 + m;
+      const uint32_t* src =
+          (const uint32_t*)((const uint8_t*)c.v + base / 2) + kb[t] * 4 * D + half * 256 + g[t] * 64 + m * 4 + ct;
+      if (kb[t] < blocks) {
+        w[t][0] = src[0], w[t][1] = src[4];
+        sc[t] = *(const cu32x2*)(c.vs + base / 32 + kb[t] * D + (g[t] * (D / 32) + (ch[t] >> 5)) * 8);
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    if (kb[t] >= blocks) continue;
+    if constexpr (FP4) {
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const cbf16x8 y = fp4_eight(w[t][z], 1.0f);
+        // a power of two times an e2m1 value: exact in bf16
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          x[t][z][j] = (__bf16)(float(y[j]) * scale_of((sc[t][j >> 2] >> (8 * (j & 3))) & 255u));
+      }
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int r = kb * 32 + (j >> 2) * 16 + g * 4 + (j & 3);
-      if (r < n) rows[r * R + ch] = x[j];
+      const int r = kb[t] * 32 + (j >> 2) * 16 + g[t] * 4 + (j & 3);
+      const __bf16 a = x[t][0][j], b = x[t][1][j];
+      const uint32_t two = uint32_t(__builtin_bit_cast(uint16_t, a)) | uint32_t(__builtin_bit_cast(uint16_t, b)) << 16;
+      if (r < n) *(uint32_t*)(rows + r * R + ch[t]) = two;
     }
   }
 }
@@ -321,7 +353,7 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
     if (vside && r0 >= r1) return;
     __bf16* rows = piece - p0 * R;
     if (!vside) {
-      stage_k<D, FP4>(a.c, phys, h, p0, min(lo, p0 + kPiece), piece);
+      stage_k<D, FP4, 1>(a.c, phys, h, p0, min(lo, p0 + kPiece), piece);
       for (int i = tid; i < (r1 - r0) * U; i += kThreads) {
         const int r = r0 + i / U, u = i % U;
         const int64_t t = tok0 + r;
@@ -477,7 +509,9 @@ struct ReadArgs {
 };
 
 // A workgroup copies 64 tokens of a page of one head and side: fragments to LDS rows to raster
-// rows (of larger pieces too few fit a CU: 128 tokens 61 us for 25385 tokens x 8 heads).
+// rows. 27673 tokens x 8 heads of 128 in 4 bits, 143 MB: 27 us (5.3 TB/s); with V turned a channel
+// at a time, each load waiting for its write, 46, and with 128 tokens a workgroup, fewer of which
+// fit a CU, 61.
 template <int D, bool FP4>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(ReadArgs a) {
   constexpr int R = lds_row<D>();
@@ -495,7 +529,7 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(ReadArgs a) {
   const int phys = a.b.table[bj];
   if (phys < 0 || phys >= a.c.n_pages) return;
   if (vside) stage_v<D, FP4>(a.c, phys, h, from, n, rows);
-  else stage_k<D, FP4>(a.c, phys, h, from, n, rows);
+  else stage_k<D, FP4, 4>(a.c, phys, h, from, n, rows);
   __syncthreads();
   __bf16* dst = (vside ? a.v : a.k) + ((int64_t(b) * a.c.H + h) * a.N + int64_t(j) * P + from) * D;
   for (int i = threadIdx.x; i < (n - from) * (D / 8); i += kThreads) {
