@@ -386,7 +386,9 @@ class CachePath:
     (topk > 0) and attention on one stream, with no host sync. A captured graph
     of `run` serves every later plan with the same number of new tokens and pages enough,
     since all buffers stay where they are. Pages go back to the pool by `release(b)`;
-    `rewind(b, length)` drops a sequence's last tokens (their pages stay reserved).
+    `rewind(b, length)` drops a sequence's last tokens (their pages stay reserved). Both write
+    the sequence's new length on torch's current stream, as `plan` does, and `run` then waits
+    for another plan.
 
     rope: None or (cos, sin) tables; positions are the tokens' places in their sequences
     unless `run` is given others (raster numbers of a `grid_rope` table)."""
@@ -415,6 +417,7 @@ class CachePath:
         self.pages = [[] for _ in range(B)]
         self.length = [0] * B
         self.n_tokens = 0
+        self.planned = True   # the device's lengths are those of the last plan
         self.q = e(max_tokens, Hq, d)
         self.counts = e(max_tokens, H, dt=torch.int32) if topk else None
         self.indices = e(max_tokens, H, topk, dt=torch.int32) if topk else None
@@ -449,6 +452,7 @@ class CachePath:
             self.length[b] += n
             cu.append(cu[-1] + n)
         self.n_tokens = cu[-1]
+        self.planned = True
         self.lens.copy_(torch.tensor(self.length, dtype=torch.int32))
         self.cu.copy_(torch.tensor(cu, dtype=torch.int32))
 
@@ -456,19 +460,26 @@ class CachePath:
         """Sequence b keeps its first `length` tokens."""
         if not 0 <= length <= self.length[b]:
             raise ValueError(f"length must lie in [0, {self.length[b]}]")
-        self.length[b] = int(length)
+        self._shorten(b, length)
 
     def release(self, b: int):
         """Sequence b starts anew; its pages return to the pool."""
         self.free += reversed(self.pages[b])
         self.pages[b] = []
-        self.length[b] = 0
+        self._shorten(b, 0)
+
+    def _shorten(self, b: int, length: int):
+        self.length[b] = int(length)
+        self.lens[b] = int(length)   # read() follows the device's lengths
+        self.planned = False
 
     def batch(self):
         return S.batch(self.table, self.lens, self.cu, self.n_tokens)
 
     def run(self, q, k, v, out=None, lse=None, pos=None, stream=None):
         """q [n, Hq, d], k, v [n, H, d], bf16, the planned tokens in sequence order -> [n, Hq, d]."""
+        if not self.planned:
+            raise ValueError("a sequence was shortened: plan() comes before run()")
         n, b = self.n_tokens, self.batch()
         if out is None:
             out = torch.empty(n, self.Hq, self.d, dtype=torch.bfloat16, device=self.device)
