@@ -391,7 +391,10 @@ class CachePath:
     for another plan.
 
     rope: None or (cos, sin) tables; positions are the tokens' places in their sequences
-    unless `run` is given others (raster numbers of a `grid_rope` table)."""
+    unless `run` is given others (raster numbers of a `grid_rope` table).
+
+    stream: a torch stream or a raw handle, torch's current stream if None. Tensors that `run`
+    and `read` make for their results are made on it."""
 
     def __init__(self, B, Hq, H, d, n_pages, max_pages, max_tokens, page=64, fp4=False, topk=0,
                  sink=0, local=1, causal=True, scale=None, rope=None, interleaved=False,
@@ -476,13 +479,23 @@ class CachePath:
     def batch(self):
         return S.batch(self.table, self.lens, self.cu, self.n_tokens)
 
+    def _on(self, stream):
+        """Makes `stream` torch's current one: memory that was freed on another stream may still
+        have work queued there, and a fill has to come before the call that it is for."""
+        if stream is not None and not isinstance(stream, torch.cuda.Stream):
+            handle = int(getattr(stream, "cuda_stream", stream))
+            stream = (torch.cuda.ExternalStream(handle, device=self.device) if handle
+                      else torch.cuda.default_stream(self.device))
+        return torch.cuda.stream(stream)  # None: no change
+
     def run(self, q, k, v, out=None, lse=None, pos=None, stream=None):
         """q [n, Hq, d], k, v [n, H, d], bf16, the planned tokens in sequence order -> [n, Hq, d]."""
         if not self.planned:
             raise ValueError("a sequence was shortened: plan() comes before run()")
         n, b = self.n_tokens, self.batch()
         if out is None:
-            out = torch.empty(n, self.Hq, self.d, dtype=torch.bfloat16, device=self.device)
+            with self._on(stream):
+                out = torch.empty(n, self.Hq, self.d, dtype=torch.bfloat16, device=self.device)
         rope = None
         if self.rope_tables is not None:
             rope = S.rope(*self.rope_tables, pos, interleaved=self.interleaved)
@@ -501,7 +514,8 @@ class CachePath:
     def read(self, N=None, stream=None):
         """Keys and values of all sequences as raster tensors [B, H, N, d], zero behind a sequence."""
         N = max(self.length) if N is None else N
-        k = torch.zeros(self.B, self.H, N, self.d, dtype=torch.bfloat16, device=self.device)
-        v = torch.zeros_like(k)
+        with self._on(stream):
+            k = torch.zeros(self.B, self.H, N, self.d, dtype=torch.bfloat16, device=self.device)
+            v = torch.zeros_like(k)
         S.spade_cache_read(self.cache, self.batch(), k, v, stream=stream)
         return k, v
