@@ -403,7 +403,8 @@ class CachePath:
         self.topk, self.sink, self.local, self.causal = topk, sink, local, causal
         self.scale = 1.0 / math.sqrt(d) if scale is None else scale
         self.rope_tables, self.interleaved = rope, interleaved
-        dev = self.device = torch.device(device)
+        self.cu = torch.zeros(B + 1, dtype=torch.int32, device=device)
+        dev = self.device = self.cu.device  # with its index: another device may be current later
         e = lambda *s, dt=torch.bfloat16: torch.empty(s, dtype=dt, device=dev)  # noqa: E731
         fmt = S.SPADE_CACHE_FP4 if fp4 else S.SPADE_CACHE_BF16
         rows, dt = (d // 2, torch.uint8) if fp4 else (d, torch.bfloat16)
@@ -414,7 +415,6 @@ class CachePath:
         self.cache = S.cache(fmt, H, d, page, self.k, self.v, self.k_mean, self.k_scale, self.v_scale)
         self.table = torch.zeros(B, max_pages, dtype=torch.int32, device=dev)
         self.lens = torch.zeros(B, dtype=torch.int32, device=dev)
-        self.cu = torch.zeros(B + 1, dtype=torch.int32, device=dev)
         self.max_pages, self.max_tokens = max_pages, max_tokens
         self.free = list(range(n_pages - 1, -1, -1))
         self.pages = [[] for _ in range(B)]

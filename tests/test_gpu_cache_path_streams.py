@@ -62,3 +62,9 @@ def test_the_default_stream_by_its_handle():
     got = p.run(*x, stream=torch.cuda.default_stream().cuda_stream)
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+def test_a_path_names_its_device():
+    """Made on "cuda", a path stays on the device that was current then."""
+    p, _ = _filled()
+    assert p.device == p.k.device and p.device.index == torch.cuda.current_device()
