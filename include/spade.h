@@ -680,8 +680,10 @@ spade_status spade_cache_select(const spade_cache* c, const spade_batch* b, cons
  *   workspace: spade_cache_attn_workspace_bytes bytes, 16-byte aligned; serves one call
  *            at a time (it holds partial results where few rows are split over the chip).
  *   bf16 MFMA with fp32 accumulation; softmax in fp32; P rounded to bf16 for the P*V
- *   product. Tokens that a query does not see never reach its result, whatever they
- *   hold. Deterministic.
+ *   product. Weights are 1 at most and divided by their sum at the end: results are
+ *   finite where the number of visible tokens times their largest |v| is below 2^127
+ *   (values below 2^-110 lose bits to underflow). Tokens that a query does not see never
+ *   reach its result, whatever they hold. Deterministic.
  */
 spade_status spade_cache_attn(const spade_cache* c, const spade_batch* b, const void* q, int32_t Hq,
                               const int32_t* counts, const int32_t* indices, int32_t topk,

@@ -11,7 +11,10 @@
 // both operands as the instruction reads them (cache.h), so a fragment is one contiguous
 // load straight into registers: no LDS, no shuffle, no transpose on the way.
 //
-// Scores, the running maximum and sum, and O are fp32. P is rounded to bf16 for the
+// A row's reference m is set 2^8 above its maximum and raised only when that passes it, so
+// weights are 1 at most: sums of them times V stay finite while keys x |V| < 2^127.
+//
+// Scores, the reference, the sum, and O are fp32. P is rounded to bf16 for the
 // product with V (as in the block-sparse attention). 4-bit keys become bf16 exactly
 // (e2m1 times a power of two); for V the power of two is moved into P, whose bf16
 // rounding it commutes with.
@@ -42,7 +45,7 @@ constexpr int kMinUnits = 16;      // units a split is worth: its start and join
 // 2048 200; two of 131072 in bf16: 384 108, 512 106, 768 and more 117.
 template <int D, bool FP4>
 constexpr int target_wgs() { return kCUs * (D == 128 && !FP4 ? 2 : 3); }
-constexpr float kLazy = 8.0f;      // the running maximum is raised when a row's grew by 2^8
+constexpr float kLazy = 8.0f;      // a row's reference lies up to 2^8 above its largest score
 
 // What a work item covers.
 struct Tile {
@@ -112,7 +115,7 @@ __device__ __forceinline__ float sum16(float v) {
   return v + __shfl_xor(v, 32);
 }
 
-// Factor that takes a partial result with maximum m to maximum `top`. A part without a key
+// Factor that takes a partial result with reference m to reference `top`. A part without a key
 // (m = -inf) holds zeros, or the NaN of scores that are none: passed on as it is.
 __device__ __forceinline__ float lift(float m, float top) {
   return m == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m - top);
@@ -168,7 +171,7 @@ struct Wave {
   static constexpr int KK = D / 32, CT = D / 16;
   cbf16x8 q[KK];
   cf32x4 o[CT];
-  float m, l;  // running maximum (base-2 logits) and this lane's share of the sum
+  float m, l;  // reference (base-2 logits) and this lane's share of the sum
 };
 
 // The rows' query fragments: the K product's channel order (contiguous pieces of d / 4
@@ -217,8 +220,8 @@ __device__ __forceinline__ void step_unit(UnitLoad<D, FP4>& u, Wave<D, FP4>& w, 
   top = max16(top) * scale2;
   top = row_in ? top : kNegInf;
   float m = w.m;
-  if (__any(top > m + kLazy)) {
-    m = top > m + kLazy ? top : m;
+  if (__any(top > m)) {
+    m = top > m ? top + kLazy : m;
     const float alpha = w.m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(w.m - m);
 #pragma unroll
     for (int c = 0; c < CT; ++c) w.o[c] *= alpha;

@@ -7,7 +7,7 @@
 // LDS for the four waves, in the pages' fragment order, which is free of bank conflicts
 // and needs no transpose. A wave skips the pages none of its own tokens keeps. The scores
 // of a page that only some of its rows keep cost nothing to mask: a row's bias is its
-// running maximum, or infinity where the row does not keep the page.
+// reference, or infinity where the row does not keep the page.
 //
 // bf16 units go from memory to LDS directly, into a ring that runs three units ahead of the
 // computation: what other workgroups have not yet brought to L2 takes longer than
@@ -15,8 +15,7 @@
 // bf16 one unit ahead, once for four waves (V's powers of two are applied there: exact).
 //
 // S^T (32 keys x 32 rows) = K Q^T and O^T += V^T P^T with mfma 32x32x16. The lane's scores
-// are then in the order in which a V fragment holds its keys. Softmax as in cache_attn.hip;
-// the running maximum is raised only when a row's grows by more than 2^8.
+// are then in the order in which a V fragment holds its keys. Softmax as in cache_attn.hip.
 //
 // Where heads are few, calls that read all tokens share a tile's pages between workgroups and
 // join the parts (cache_attn.hip, which chooses).
@@ -41,7 +40,7 @@ constexpr int kWaves = kChunkWaves;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kTileRows = kChunkRows * kWaves;
 constexpr int kSeg = 512;          // pages walked before the masks are built anew
-constexpr float kLazy = 8.0f;
+constexpr float kLazy = 8.0f;      // see cache_attn.hip
 
 // LDS of the walk. bf16: a ring of units that are on their way or in use. 4 bits: a ring of
 // units as they lie in the page, and two widened ones.
@@ -134,7 +133,7 @@ template <int D>
 struct Rows {
   cbf16x8 q[D / 16];
   f32x16 o[D / 32];
-  float m, l;
+  float m, l;  // reference and this lane's share of the sum
 };
 
 // One staged unit, keys at..at+31. row_in: the lane's row keeps the page. edge (the same for all
@@ -175,8 +174,8 @@ __device__ __forceinline__ void step(const char* kf, const char* vf, Rows<D>& w,
   top = row_max(top) * scale2;
   top = row_in ? top : kNegInf;
   float m = w.m;
-  if (__any(top > m + kLazy)) {
-    m = top > m + kLazy ? top : m;
+  if (__any(top > m)) {
+    m = top > m ? top + kLazy : m;
     const float alpha = w.m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(w.m - m);
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) w.o[c] *= alpha;
