@@ -546,8 +546,10 @@ spade_status spade_sparse_attn_raster_multi(const spade_geom* geoms, int32_t n_g
  *   - A page that receives tokens belongs to one sequence; full pages may be shared.
  *   - Limits: d in {64, 128}; page a multiple of 32 in [32, 256]; H <= 4096;
  *     Hq / H <= 128; n_pages * page < 2^31; B <= 2^20; n_tokens <= 2^28; max_pages <=
- *     2^23, and <= 16384 for selections and attention with lists. B or n_tokens equal
- *     to 0 is an empty problem.
+ *     2^23, and <= 16384 for selections and attention with lists; max_pages * page <=
+ *     2^30 for attention; B * max_pages < 2^31 for the read-back. Beyond them, and for
+ *     2^31 workgroups or more, SPADE_ERR_UNSUPPORTED. B or n_tokens equal to 0 is an
+ *     empty problem.
  */
 enum { SPADE_CACHE_BF16 = 0, SPADE_CACHE_FP4 = 1 };  /* formats of a cache */
 

@@ -810,8 +810,9 @@ spade_status spade_cache_read(const spade_cache* c, const spade_batch* b, int64_
     return fail(SPADE_ERR_INVALID_ARG, "k, v (two tensors), table and lens must be non-null");
   if (!aligned16(k) || !aligned16(v))
     return fail(SPADE_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
-  if (int64_t(b->B) * b->max_pages > 0x7fffffff / (c->H * 2) / ((c->page + 63) / 64))
-    return fail(SPADE_ERR_UNSUPPORTED, "batch too large (B * max_pages * H)");
+  if (int64_t(b->B) * b->max_pages > 0x7fffffff ||
+      int64_t(b->B) * spade::cache_read_pages(dc, db, N) > 0x7fffffff / (c->H * 2) / ((c->page + 63) / 64))
+    return fail(SPADE_ERR_UNSUPPORTED, "batch too large (B * max_pages, or B * H * N)");
   return hip_status(spade::launch_cache_read(dc, db, c->d, N, k, v, stream), "cache read launch");
 }
 

@@ -49,6 +49,11 @@ hipError_t launch_cache_append(const DevCache& c, const DevBatch& b, int d, cons
                                const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                                const void* q, int64_t q_stride, int Hq, void* q_out,
                                hipStream_t s);
+// Pages of a sequence that N tokens take.
+inline int cache_read_pages(const DevCache& c, const DevBatch& b, int64_t N) {
+  const int64_t pages = (N + c.page - 1) / c.page;
+  return int(pages < b.max_pages ? pages : b.max_pages);
+}
 hipError_t launch_cache_read(const DevCache& c, const DevBatch& b, int d, int64_t N, void* k,
                              void* v, hipStream_t s);
 
@@ -88,6 +93,23 @@ typedef float cf32x4 __attribute__((ext_vector_type(4)));
 typedef float cf32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t cu32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t cu32x2 __attribute__((ext_vector_type(2)));
+
+// Launches workgroups 0..wgs-1 (fewer than 2^31) of a kernel whose arguments have a member
+// `first`. A launch counts its threads in 32 bits: larger ones go in parts, each told its first
+// workgroup.
+template <typename Args>
+hipError_t launch_parts(void (*kernel)(Args), Args a, int64_t wgs, int rows, int threads, int lds,
+                        hipStream_t s) {
+  const int64_t most = (int64_t(1) << 32) / threads - 8;  // a multiple of 8: XCDs keep their turns
+  for (int64_t first = 0; first < wgs; first += most) {
+    const int64_t n = wgs - first < most ? wgs - first : most;
+    a.first = uint32_t(first);
+    kernel<<<dim3(unsigned(n), unsigned(rows)), threads, lds, s>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
 
 // Work items cut from a batch: sequence b's new tokens cu[b]..cu[b+1]-1 fill at most
 // floor(cu[b+1] / unit) - floor(cu[b] / unit) + extra items, a sum that telescopes, so

@@ -264,6 +264,7 @@ struct AppendArgs {
   int64_t k_stride, v_stride, q_stride;
   int Hq;
   int64_t page_wgs;  // the first workgroups: for each (page item, head) K, then V in pieces
+  uint32_t first;    // of the launch
 };
 
 template <int D, bool FP4>
@@ -274,7 +275,7 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
   __shared__ __attribute__((aligned(16))) char lds[kPiece * R * 2];
   static_assert(sizeof(lds) >= (kCuLds + 1) * sizeof(int) && sizeof(lds) >= 2 * kThreads * sizeof(double), "");
   __bf16* piece = (__bf16*)lds;
-  const int64_t wg = blockIdx.x;
+  const int wg = int(a.first + blockIdx.x);
   const int tid = threadIdx.x;
 
   if (wg >= a.page_wgs) {  // queries: a thread turns one unit of kHeads neighbouring heads
@@ -324,11 +325,10 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
   }
 
   const int P = a.c.page, sides = 1 + (P + kPiece - 1) / kPiece;  // K, and V in pieces
-  const int64_t ih = wg / sides;
-  const int side = int(wg - ih * sides);
+  const int ih = wg / sides, side = wg - ih * sides;
   const bool vside = side > 0;
-  const int h = int(ih % a.c.H);
-  const SeqItem it = find_item(a.b, int(ih / a.c.H), P, 2);
+  const int h = ih % a.c.H;
+  const SeqItem it = find_item(a.b, ih / a.c.H, P, 2);
   if (it.b < 0) return;
   const int64_t len = it.len;
   const int64_t start = len - it.n;  // place of the first new token
@@ -501,6 +501,8 @@ __global__ void __launch_bounds__(kThreads) cache_append_kernel(AppendArgs a) {
 }
 
 struct ReadArgs {
+  uint32_t first;  // workgroup of the launch
+  int pages;       // of a sequence, at most
   DevCache c;
   DevBatch b;
   __bf16* k;
@@ -516,17 +518,16 @@ template <int D, bool FP4>
 __global__ void __launch_bounds__(kThreads) cache_read_kernel(ReadArgs a) {
   constexpr int R = lds_row<D>();
   __shared__ __attribute__((aligned(16))) __bf16 rows[kPiece * R];
-  const int64_t wg = blockIdx.x;
+  const int wg = int(a.first + blockIdx.x);
   const bool vside = wg & 1;
   const int P = a.c.page, pieces = (P + kPiece - 1) / kPiece;
-  const int from = int((wg >> 1) % pieces) * kPiece;
-  const int64_t bjh = (wg >> 1) / pieces, bj = bjh / a.c.H;
-  const int h = int(bjh - bj * a.c.H);
-  const int b = int(bj / a.b.max_pages), j = int(bj - int64_t(b) * a.b.max_pages);
+  const int from = (wg >> 1) % pieces * kPiece;
+  const int bjh = (wg >> 1) / pieces, bj = bjh / a.c.H, h = bjh - bj * a.c.H;
+  const int b = bj / a.pages, j = bj - b * a.pages;
   const int64_t to = min(int64_t(a.b.lens[b]), a.N);
   const int n = int(min(to - int64_t(j) * P, int64_t(min(P, from + kPiece))));
   if (n <= from) return;
-  const int phys = a.b.table[bj];
+  const int phys = a.b.table[int64_t(b) * a.b.max_pages + j];
   if (phys < 0 || phys >= a.c.n_pages) return;
   if (vside) stage_v<D, FP4>(a.c, phys, h, from, n, rows);
   else stage_k<D, FP4, 4>(a.c, phys, h, from, n, rows);
@@ -536,19 +537,6 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(ReadArgs a) {
     const int r = i / (D / 8), x = i % (D / 8);
     *(cu32x4*)(dst + int64_t(i) * 8) = *(cu32x4*)(rows + r * R + x * 8);
   }
-}
-
-template <int D, bool FP4>
-hipError_t append(const AppendArgs& a, int64_t wgs, hipStream_t s) {
-  cache_append_kernel<D, FP4><<<dim3(unsigned(wgs)), kThreads, 0, s>>>(a);
-  return hipGetLastError();
-}
-
-template <int D, bool FP4>
-hipError_t read(const ReadArgs& a, hipStream_t s) {
-  const int64_t wgs = int64_t(a.b.B) * a.b.max_pages * a.c.H * 2 * ((a.c.page + kPiece - 1) / kPiece);
-  cache_read_kernel<D, FP4><<<dim3(unsigned(wgs)), kThreads, 0, s>>>(a);
-  return hipGetLastError();
 }
 
 }  // namespace
@@ -572,8 +560,9 @@ hipError_t launch_cache_append(const DevCache& c, const DevBatch& b, int d, cons
   a.page_wgs = int64_t(item_base(b.n_tokens, b.B, c.page, 2)) * c.H * (1 + (c.page + kPiece - 1) / kPiece);
   const int64_t units = q ? int64_t(b.n_tokens) * ((Hq + kHeads - 1) / kHeads) * (d / 16) : 0;
   const int64_t wgs = a.page_wgs + (units + kThreads - 1) / kThreads;
-  if (d == 128) return c.fp4 ? append<128, true>(a, wgs, s) : append<128, false>(a, wgs, s);
-  return c.fp4 ? append<64, true>(a, wgs, s) : append<64, false>(a, wgs, s);
+  const auto kernel = d == 128 ? (c.fp4 ? cache_append_kernel<128, true> : cache_append_kernel<128, false>)
+                               : (c.fp4 ? cache_append_kernel<64, true> : cache_append_kernel<64, false>);
+  return launch_parts(kernel, a, wgs, 1, kThreads, 0, s);
 }
 
 hipError_t launch_cache_read(const DevCache& c, const DevBatch& b, int d, int64_t N, void* k,
@@ -584,8 +573,11 @@ hipError_t launch_cache_read(const DevCache& c, const DevBatch& b, int d, int64_
   a.k = (__bf16*)k;
   a.v = (__bf16*)v;
   a.N = N;
-  if (d == 128) return c.fp4 ? read<128, true>(a, s) : read<128, false>(a, s);
-  return c.fp4 ? read<64, true>(a, s) : read<64, false>(a, s);
+  a.pages = cache_read_pages(c, b, N);
+  const int64_t wgs = int64_t(b.B) * a.pages * c.H * 2 * ((c.page + kPiece - 1) / kPiece);
+  const auto kernel = d == 128 ? (c.fp4 ? cache_read_kernel<128, true> : cache_read_kernel<128, false>)
+                               : (c.fp4 ? cache_read_kernel<64, true> : cache_read_kernel<64, false>);
+  return launch_parts(kernel, a, wgs, 1, kThreads, 0, s);
 }
 
 }  // namespace spade

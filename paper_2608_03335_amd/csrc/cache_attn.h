@@ -28,6 +28,7 @@ struct AttnArgs {
   int64_t items;            // tiles of all sequences, at most
   int splits;               // most workgroups that share a tile's walk
   int wgs;                  // workgroups a call is split into, about
+  uint32_t first;           // workgroup of the launch
 };
 
 // Many queries a sequence: tiles of 128 rows, four waves of 32, that share staged keys

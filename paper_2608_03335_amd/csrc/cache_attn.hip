@@ -348,8 +348,9 @@ __global__ void __launch_bounds__(kThreads, FP4 ? 3 : 2) cache_attn_kernel(AttnA
   extern __shared__ __attribute__((aligned(16))) char lds[];
   __shared__ float ml[kWaves][16][2];
   const int ny = a.c.H * a.RT;
-  const int per = int(a.items), y = blockIdx.x % ny;
-  const int split = blockIdx.x / ny / per, tile = blockIdx.x / ny % per;
+  const uint32_t wg = a.first + blockIdx.x;
+  const int per = int(a.items), y = wg % ny;
+  const int split = wg / ny / per, tile = wg / ny % per;
   Tile t;
   const bool any = find_tile(a, tile, y, &t);
   if (a.splits > 1 && split == 0 && threadIdx.x == 0)
@@ -490,14 +491,15 @@ template <int D, int ROWS, int GROUP>
 __global__ void __launch_bounds__(kThreads) cache_join_kernel(AttnArgs a) {
   constexpr int PIECES = D / 4, RUNS = 64 / PIECES, AHEAD = 8;
   constexpr int64_t STRIDE = ROWS * (D + 2);
-  const JoinHead t = a.join[blockIdx.x];
+  const uint32_t tile = a.first + blockIdx.x;
+  const JoinHead t = a.join[tile];
   if (t.splits <= 1) return;
   const int lane = threadIdx.x & 63, c4 = lane % PIECES, run = lane / PIECES;
   const int row = blockIdx.y * kWaves + (threadIdx.x >> 6);
   const int in_group = row % GROUP, q = in_group / t.heads, gh = in_group - q * t.heads;
   const int per_group = GROUP / t.heads, rq = row / GROUP * per_group + q;
   if (q >= per_group || rq >= t.nq) return;
-  const float* po = a.part + int64_t(blockIdx.x) * a.splits * STRIDE;
+  const float* po = a.part + int64_t(tile) * a.splits * STRIDE;
   // loads of the partial results a batch ahead of their use, the first ahead of the statistics
   cf32x4 next[AHEAD];
   auto fetch = [&](int s0) {
@@ -606,22 +608,17 @@ hipError_t run(const AttnArgs& a, const Plan& p, hipStream_t s) {
                                             kCacheMaxPages * 4 + kWaves * 16 * (D + 4) * 4);
     if (e != hipSuccess) return e;
   }
-  const int64_t tiles = p.items * a.c.H * p.RT;
-  cache_attn_kernel<D, FP4><<<dim3(unsigned(tiles * p.splits)), kThreads, p.lds, s>>>(a);
-  return hipGetLastError();
+  return launch_parts(cache_attn_kernel<D, FP4>, a, p.items * a.c.H * p.RT * p.splits, 1, kThreads, p.lds, s);
 }
 
 template <int D>
 hipError_t join(const AttnArgs& a, const Plan& p, hipStream_t s) {
-  const unsigned tiles = unsigned(p.items * a.c.H * p.RT);
-  if (p.chunk) {
-    cache_join_kernel<D, kChunkRows * kChunkWaves, kChunkRows>
-        <<<dim3(tiles, kChunkRows * kChunkWaves / kWaves), kThreads, 0, s>>>(a);
-  } else {
-    const int rows = p.QT * (p.G < 16 ? p.G : 16);
-    cache_join_kernel<D, 16, 16><<<dim3(tiles, (rows + kWaves - 1) / kWaves), kThreads, 0, s>>>(a);
-  }
-  return hipGetLastError();
+  const int64_t tiles = p.items * a.c.H * p.RT;
+  if (p.chunk)
+    return launch_parts(cache_join_kernel<D, kChunkRows * kChunkWaves, kChunkRows>, a, tiles,
+                        kChunkRows * kChunkWaves / kWaves, kThreads, 0, s);
+  const int rows = p.QT * (p.G < 16 ? p.G : 16);
+  return launch_parts(cache_join_kernel<D, 16, 16>, a, tiles, (rows + kWaves - 1) / kWaves, kThreads, 0, s);
 }
 
 }  // namespace

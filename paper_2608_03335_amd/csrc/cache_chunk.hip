@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, 2) cache_chunk_kernel(AttnArgs a) {
   __shared__ Seg sg;
   // each XCD takes a run of neighbouring items of a head and split: they want the same pages
   const int64_t items = a.items, total = items * a.c.H * a.splits, per = (total + 7) >> 3;
-  const int64_t slot = blockIdx.x >> 3, L = (blockIdx.x & 7) * per + slot;
+  const int64_t wg = a.first + blockIdx.x, slot = wg >> 3, L = (wg & 7) * per + slot;
   if (slot >= per || L >= total) return;
   const int hs = int(L / items), item = int(L - hs * items), h = hs / a.splits, split = hs - h * a.splits;
   JoinHead* head = a.join + int64_t(item) * a.c.H + h;
@@ -431,8 +431,7 @@ hipError_t run(const AttnArgs& a, hipStream_t s) {
     if (e != hipSuccess) return e;
   }
   const int64_t wgs = (a.items * a.c.H * a.splits + 7) / 8 * 8;
-  cache_chunk_kernel<D, FP4><<<dim3(unsigned(wgs)), kThreads, bytes, s>>>(a);
-  return hipGetLastError();
+  return launch_parts(cache_chunk_kernel<D, FP4>, a, wgs, 1, kThreads, bytes, s);
 }
 
 }  // namespace
