@@ -128,10 +128,11 @@ __host__ __device__ inline int item_base(int tokens, int b, int unit, int extra)
 }
 
 // Finds the sequence of a work item among the tokens from..to-1: every thread of the block
-// looks at some sequences, so the search and the sequence's length cost one load latency
-//. All threads of
-// the block must call. Offsets that do not ascend cannot lead out of the batch's arrays: an
-// item then belongs to one of the sequences that claim it, or to none.
+// looks at some sequences, so the search and the sequence's length cost one load latency; of
+// more than kScan sequences, a load latency more for each factor of the block's threads. All
+// threads of the block must call. Offsets that do not ascend cannot lead out of the batch's
+// arrays: an item then belongs to one of the sequences that claim it, or to none.
+constexpr int kScan = 1024;
 __device__ __forceinline__ SeqItem find_item(const DevBatch& bt, int item, int unit, int extra,
                                              int from, int to) {
   __shared__ int hit, info[5];
@@ -141,7 +142,19 @@ __device__ __forceinline__ SeqItem find_item(const DevBatch& bt, int item, int u
   r.b = -1;
   r.len = 0;
   r.start = r.all = r.t0 = r.n = 0;
-  for (int b = threadIdx.x; b < bt.B; b += blockDim.x) {
+  int b0 = 0, n = bt.B;  // the item's sequence is one of b0..b0+n-1: the last that begins before it
+  while (n > kScan) {
+    const int step = (n + blockDim.x - 1) / blockDim.x, at = int(threadIdx.x) * step;
+    bool before = false;
+    if (at < n) {
+      const int start = min(max(bt.cu[b0 + at], 0), bt.n_tokens);
+      before = item_base(min(max(start, from), to) - from, b0 + at, unit, extra) <= item;
+    }
+    const int skip = max(__syncthreads_count(before) - 1, 0) * step;
+    b0 += skip;
+    n = min(n - skip, step);
+  }
+  for (int b = b0 + threadIdx.x; b < b0 + n; b += blockDim.x) {
     const int start = min(max(bt.cu[b], 0), bt.n_tokens), end = min(max(bt.cu[b + 1], 0), bt.n_tokens);
     const int len = bt.lens[b];
     const int lo = min(max(start, from), to), hi = min(max(end, from), to);

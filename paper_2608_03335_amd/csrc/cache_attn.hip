@@ -39,6 +39,8 @@ constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kMaxSplits = 64;
 constexpr int kCUs = 256;
+constexpr int64_t kMaxIdle = 65536;  // workgroups of a split call, tiles without tokens among them
+constexpr int kMaxShared = 4096;   // sequences of a split call
 constexpr int kMinUnits = 16;      // units a split is worth: its start and join cost as much
 // Workgroups that are on the card at once (256 CUs, by registers): a call is split into about
 // as many. On 64 4-bit contexts of up to 16384 tokens: 384 186 us, 512 183, 768 175, 1024 177,
@@ -595,6 +597,10 @@ Plan plan(const DevCache& c, const DevBatch& b, int d, int Hq, int topk) {
   // workgroups without splits: tiles that hold tokens (at most), heads, row tiles
   const int64_t wgs = (p.QT > 1 ? b.n_tokens / p.QT + holders : b.n_tokens) * c.H * p.RT;
   p.splits = splits_of(2 * p.wgs + wgs - 1, wgs, walk(each < p.QT ? each : p.QT), c.page, kMinUnits);
+  // tiles of sequences without tokens are as many for each split, and a split call's workgroups
+  // add up all sequences
+  const int64_t idle = kMaxIdle / (p.items * c.H * p.RT);
+  p.splits = b.B > kMaxShared || idle < 1 ? 1 : int(p.splits < idle ? p.splits : idle);
   p.lds = kWaves * 16 * (d + 4) * 4 + (topk ? (b.max_pages * 4 + 15) / 16 * 16 : 0);
   return p;
 }

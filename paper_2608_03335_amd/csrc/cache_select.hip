@@ -281,12 +281,20 @@ __global__ void __launch_bounds__(W == 16 ? 1024 : kThreads) cache_topk_kernel(S
   const int64_t rows = int64_t(a.t1 - a.t0) * a.c.H;
   if (r >= rows) return;  // W > 1: one row a workgroup, all waves leave
   const int t = a.t0 + int(r / a.c.H), h = int(r % a.c.H);
-  // the row's sequence: a lane looks at every 64th
+  // the row's sequence: a lane looks at every 64th (of many: at every 64th of those that are left)
   int b = -1, lo = 0, vis = 0;
-  for (int b0 = 0; b0 < a.b.B && b < 0; b0 += 64) {
+  int first_b = 0, n_b = a.b.B;  // one of first_b..first_b+n_b-1: the last that begins before t
+  while (n_b > kScan / 4) {
+    const int step = (n_b + 63) / 64, at = lane * step;
+    const bool before = at < n_b && min(max(a.b.cu[first_b + at], 0), a.b.n_tokens) <= t;
+    const int skip = max(__popcll(__ballot(before)) - 1, 0) * step;
+    first_b += skip;
+    n_b = min(n_b - skip, step);
+  }
+  for (int b0 = first_b; b0 < first_b + n_b && b < 0; b0 += 64) {
     const int i = b0 + lane;
     int start = 0, end = 0, len = 0;
-    if (i < a.b.B) {
+    if (i < first_b + n_b) {
       start = min(max(a.b.cu[i], 0), a.b.n_tokens);
       end = min(max(a.b.cu[i + 1], 0), a.b.n_tokens);
       len = a.b.lens[i];
