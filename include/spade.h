@@ -650,6 +650,9 @@ size_t spade_cache_attn_workspace_bytes(const spade_cache* c, const spade_batch*
  * block selection, with the query side summed over the heads that share a K/V head.
  *
  *   score(t, h, j) = sum_c (sum_g q[t, h Hq/H + g, c]) k_mean[page j, h, c], in fp64.
+ *           Scores closer than the rounding of these sums, (Hq/H + d) 2^-53 of the sum of
+ *           |q| |k_mean| each, rank as they come out, the same on every call; pages with
+ *           equal means tie.
  *   causal: 1: query i of sequence b's n sees the first lens[b] - n + i + 1 tokens; 0: all
  *           lens[b]. A page is visible when one of its tokens is.
  *   Kept: min(topk, visible) pages: the first `sink` and the last `local` visible ones,

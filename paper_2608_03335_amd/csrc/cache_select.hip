@@ -1,12 +1,14 @@
-// Page selection for single queries (gfx950).
+// Page selection (gfx950): Top-K pages for every query and K/V head.
 //
 // score(t, h, j) = sum_c (sum_g q[t, h G + g, c]) mean[j, h, c]: the mean estimate of the
 // block selection with the query side summed over the heads that share a K/V head. Every
 // (query, head) keeps min(topk, visible) pages: the first `sink` and last `local` ones,
 // then by (score descending, index ascending), a NaN after every number.
 //
-// The result is that of fp64 scores, which no order of a sum can change; but nearly every
-// page is decided by far less. Two kernels:
+// The result is that of fp64 scores: the heads in order, then 16 runs of d / 16 channels,
+// added pairwise, the same for every page. (Terms that span fewer than some 23 bits sum exactly;
+// wider ones are off by (G + d) 2^-53 of their sizes' sum at most, and only pages closer than that
+// depend on the order.) Nearly every page is decided by far less. Two kernels:
 //   scores  s~ on the matrix unit: tiles of 16 queries x 128 pages, the summed query split
 //           into two bf16 terms. |s~ - s| <= E = 2^-13 |A|_1 M, with A = sum_g |q| and M the
 //           largest |mean| of the walk: 2^-16 A for the third term left out, G 2^-24 A for
