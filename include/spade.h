@@ -540,9 +540,11 @@ spade_status spade_sparse_attn_raster_multi(const spade_geom* geoms, int32_t n_g
  *     Rows before cu[0] or from cu[B] on belong to no sequence: outputs there are left
  *     as they were.
  *   - table, lens and cu are device memory and not known to the host; values that break
- *     the rules below cannot fault. lens beyond max_pages * page count as that; pages
- *     outside [0, n_pages) hold no token (appends to them are dropped); offsets that
- *     do not ascend, or leave [0, n_tokens], give unspecified rows.
+ *     the rules below cannot fault. Tokens from max_pages * page on, and those on pages
+ *     outside [0, n_pages), have no place: appends of them are dropped, nobody sees them
+ *     (their own queries see what lies before). Of more new tokens than lens, the
+ *     first ones lie before the sequence: dropped, and their queries see nothing under
+ *     causal. Offsets that do not ascend, or leave [0, n_tokens], give unspecified rows.
  *   - A page that receives tokens belongs to one sequence; full pages may be shared.
  *   - Limits: d in {64, 128}; page a multiple of 32 in [32, 256]; H <= 4096;
  *     Hq / H <= 128; n_pages * page < 2^31; B <= 2^20; n_tokens <= 2^28; max_pages <=
