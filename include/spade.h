@@ -681,7 +681,8 @@ spade_status spade_cache_select(const spade_cache* c, const spade_batch* b, cons
  *   counts, indices: int32 [n_tokens, H] and [n_tokens, H, topk]. A list is a set of pages:
  *            any order; entries that are not visible pages are skipped, an entry listed
  *            twice counts once, counts are clamped to [0, topk].
- *   q, o:    bf16 [n_tokens, Hq, d]; a query that sees no token gets o = 0, lse = -inf.
+ *   q, o:    bf16 [n_tokens, Hq, d]; a query that sees no token, or only scores of -inf, gets
+ *            o = 0, lse = -inf.
  *   lse:     out, nullable, fp32 [n_tokens, Hq]: natural log of the softmax denominator.
  *   scale:   in [1e-30, 1e30].
  *   workspace: spade_cache_attn_workspace_bytes bytes, 16-byte aligned; serves one call
@@ -690,7 +691,9 @@ spade_status spade_cache_select(const spade_cache* c, const spade_batch* b, cons
  *   product. Weights are 1 at most and divided by their sum at the end: results are
  *   finite where the number of visible tokens times their largest |v| is below 2^127
  *   (values below 2^-110 lose bits to underflow). Tokens that a query does not see never
- *   reach its result, whatever they hold. Deterministic.
+ *   reach its result, whatever they hold. The same call gives the same bits; how a
+ *   sequence's keys are divided, and with it the last bits of its results, depends on the
+ *   other sequences of the call.
  */
 spade_status spade_cache_attn(const spade_cache* c, const spade_batch* b, const void* q, int32_t Hq,
                               const int32_t* counts, const int32_t* indices, int32_t topk,
