@@ -1,4 +1,5 @@
-// Attention of single queries over the paged cache (gfx950).
+// Attention over the paged cache in tiles of 16 query rows (gfx950): single tokens, short
+// chunks, chunks under lists in few heads, and groups of more than 32 query heads.
 //
 // A work item is a tile of up to 16 query rows that share one K/V head: the G query heads
 // of one token, or of the 16 / G neighbouring tokens of one sequence when G < 16. It walks
@@ -25,9 +26,11 @@
 // that must not see it: a workgroup whose result has a NaN repeats its walk for each token
 // alone, clearing V beyond what that token sees.
 //
-// Bound by HBM where contexts are long: 64 contexts of up to 16384 tokens, 32 x 8 heads of 128
-// in 4 bits, 605 MB in 170 us (3.6 TB/s: the 4-bit conversion shares the wave's issue with the
-// loads'); two of 131072, 32 x 4 heads in bf16, 493 MB in 89 us (5.5 TB/s) and 6 for the join.
+// Bound by HBM where contexts are long: two of 131072 tokens, 32 x 4 heads of 128 in bf16, 493 MB
+// in 90 us (5.5 TB/s) and 6 for the join. In 4 bits by the chain of a unit (load, widen, product,
+// maximum, exponent, product) with too few waves to hide it: 64 contexts of up to 16384 tokens,
+// 32 x 8 heads of 128, 605 MB in 168 us (3.6 TB/s), vector instructions in 34% of the SIMDs'
+// cycles, 1.6 waves a SIMD on average where three fit, since the contexts differ in length.
 // Bound by the latency of one walk where they are short: one token over 16 pages of 64, 10 us
 // and 4 for the join.
 #include "cache_attn.h"
@@ -572,7 +575,7 @@ Plan plan(const DevCache& c, const DevBatch& b, int d, int Hq, int topk) {
   // that read all tokens split the keys of such tiles to fill it twice. Measured, in us, this side
   // and tiles of 16 rows (bf16, width 128, one sequence; Hq x H, context, new tokens):
   //   all tokens   16 x 4, 8192, 500: 61, 102    32 x 8, 16384, 200: 90, 154   64: 53, 55   24: 39, 37
-  //                12 x 12, 16384, 1200: 175, 323, and 398 without splits; 32 x 8, 4-bit, 200: 112, 165
+  //                12 x 12, 16384, 1200: 170, 323, and 398 without splits; 32 x 8, 4-bit, 200: 112, 165
   //   listed pages 32 x 8, 16384, 200, 32 pages: 78, 62    16 x 4, width 64, 4-bit, 400, 24: 49, 36
   // Lists leave a tile's rows little in common, so what fills the card is more and smaller tiles.
   const int64_t rows = int64_t(b.n_tokens) * p.G;

@@ -20,12 +20,14 @@
 // Where heads are few, calls that read all tokens share a tile's pages between workgroups and
 // join the parts (cache_attn.hip, which chooses).
 //
-// Bound by the barrier of each unit: four waves share the staged keys, and under lists wait
-// for the one that keeps a page. 4680 queries of 12 heads of 128, 40 of 512 pages each: 74
-// GFLOP in 790 us; the tiles' unions hold 5.8 times that for the matrix unit, and 355 us pass
-// with the loads alone. 4087 queries of 32 x 4 heads, 64 wide, 32 pages of 32 each in 4 bits:
-// 34 GFLOP in 167 us. All tokens, 12 heads of 128, 1200 queries of 16384 tokens: 116 GFLOP in
-// 169 us (690 TFLOP/s).
+// Bound by the series of a unit's steps (scores, softmax, P V, with a barrier in front) at two
+// workgroups a CU; under lists also by waves that wait for the one that keeps a page, and by
+// rows that do not keep it. 4680 queries of 12 heads of 128, 40 of 512 pages each: 74 GFLOP in
+// 800 us; waves of 32 rows multiply 5.8 times that, of a page that 13 of the tile's 128 rows
+// keep, and 355 us pass with the loads alone. 4087 queries of 32 x 4 heads, 64 wide, 32
+// pages of 32 each in 4 bits: 34 GFLOP in 169 us, 1.4 times the work, but 182 vector and 122 scalar
+// instructions for the eight products of a wave's unit. All tokens, 12 heads of 128, 1200
+// queries of 16384 tokens: 116 GFLOP in 170 us (685 TFLOP/s).
 //
 // What a row must not see: see cache_attn.hip.
 #include "cache_attn.h"

@@ -22,7 +22,7 @@
 //
 // Scores are bound by the means' bytes (d bf16 a page and head), in short launches by the
 // latency of one chain: offsets, table, means, product. The search makes about 20 passes over
-// a row's scores, which a wave holds in registers. Measured: 16 sequences of up to 1024 pages,
+// a row's scores, which a wave holds in registers, each waiting for the last. Measured: 16 sequences of up to 1024 pages,
 // 8 heads of 128, one query each: scores 12 us (18 MB), search 12; 3890 queries, 2 heads of
 // 64, 513 pages: 21 and 31.
 #include "cache.h"

@@ -382,10 +382,10 @@ class CachePath:
 
     Each step takes the new tokens of all sequences: `plan(new)` reserves their pages and
     writes the batch's offsets (host work and small copies on torch's current stream, which
-    has to be ordered with the stream of `run`), `run(q, k, v)` issues append, selection
-    (topk > 0) and attention on one stream, with no host sync. A captured graph
-    of `run` serves every later plan with the same number of new tokens and pages enough,
-    since all buffers stay where they are. Pages go back to the pool by `release(b)`;
+    it waits for, and which has to be ordered with the stream of `run`), `run(q, k, v)` issues
+    append, selection (topk > 0) and attention on one stream, with no host sync. A captured
+    graph of `run` serves every later plan with the same number of new tokens and pages
+    enough, since all buffers stay where they are. Pages go back to the pool by `release(b)`;
     `rewind(b, length)` drops a sequence's last tokens (their pages stay reserved). Both write
     the sequence's new length on torch's current stream, as `plan` does, and `run` then waits
     for another plan.
