@@ -786,9 +786,8 @@ spade_status spade_cache_append(const spade_cache* c, const spade_batch* b, cons
     return fail(SPADE_ERR_INVALID_ARG, "q_out may be q only where q is contiguous");
   if (r.rot && (!r.cos || !r.sin || !aligned16(r.cos) || !aligned16(r.sin)))
     return fail(SPADE_ERR_INVALID_ARG, "rope: cos and sin must be non-null and 16-byte aligned");
-  const int64_t wgs = int64_t(spade::item_base(b->n_tokens, b->B, c->page, 2)) * c->H * 5 +
-                      (int64_t(b->n_tokens) * Hq * (c->d / 16) + 255) / 256;
-  if (wgs > 0x7fffffff) return fail(SPADE_ERR_UNSUPPORTED, "batch too large (n_tokens, heads)");
+  if (!spade::cache_append_fits(dc, db, c->d, q ? Hq : 0))
+    return fail(SPADE_ERR_UNSUPPORTED, "batch too large (n_tokens, heads)");
   return hip_status(spade::launch_cache_append(dc, db, c->d, r, k, k_stride, v, v_stride, q, q_stride,
                                                Hq, q_out, stream),
                     "cache append launch");
@@ -854,6 +853,8 @@ spade_status spade_cache_select(const spade_cache* c, const spade_batch* b, cons
   if (!q || !counts || !indices || !b->table || !b->lens || !b->cu)
     return fail(SPADE_ERR_INVALID_ARG, "q, counts, indices, table, lens and cu must be non-null");
   if (!aligned16(q)) return fail(SPADE_ERR_INVALID_ARG, "q must be 16-byte aligned");
+  if (!spade::cache_select_fits(dc, db))
+    return fail(SPADE_ERR_UNSUPPORTED, "batch too large (B=%d, n_tokens=%d, H=%d)", b->B, b->n_tokens, c->H);
   const size_t need = spade::cache_select_workspace_bytes(dc, db, c->d, Hq, topk);
   if (workspace_bytes < need || (need > 0 && (workspace == nullptr || !aligned16(workspace))))
     return fail(SPADE_ERR_WORKSPACE, "16-byte aligned workspace of %zu bytes needed, %zu given", need,

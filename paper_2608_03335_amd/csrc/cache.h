@@ -45,6 +45,7 @@ struct DevRope {
   int n_pos, rot, interleaved;
 };
 
+bool cache_append_fits(const DevCache& c, const DevBatch& b, int d, int Hq);  // its grid
 hipError_t launch_cache_append(const DevCache& c, const DevBatch& b, int d, const DevRope& r,
                                const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                                const void* q, int64_t q_stride, int Hq, void* q_out,
@@ -64,6 +65,7 @@ struct CacheSelect {
   int* counts;
   int* indices;
 };
+bool cache_select_fits(const DevCache& c, const DevBatch& b);  // its grid
 size_t cache_select_workspace_bytes(const DevCache& c, const DevBatch& b, int d, int Hq, int topk);
 hipError_t launch_cache_select(const DevCache& c, const DevBatch& b, int d, const CacheSelect& p,
                                void* ws, hipStream_t s);

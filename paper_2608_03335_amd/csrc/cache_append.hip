@@ -539,7 +539,18 @@ __global__ void __launch_bounds__(kThreads) cache_read_kernel(ReadArgs a) {
   }
 }
 
+int64_t page_workgroups(const DevCache& c, const DevBatch& b) {
+  return int64_t(item_base(b.n_tokens, b.B, c.page, 2)) * c.H * (1 + (c.page + kPiece - 1) / kPiece);
+}
+int64_t query_workgroups(const DevBatch& b, int d, int Hq) {
+  return (int64_t(b.n_tokens) * ((Hq + kHeads - 1) / kHeads) * (d / 16) + kThreads - 1) / kThreads;
+}
+
 }  // namespace
+
+bool cache_append_fits(const DevCache& c, const DevBatch& b, int d, int Hq) {
+  return page_workgroups(c, b) + query_workgroups(b, d, Hq) <= 0x7fffffff;
+}
 
 hipError_t launch_cache_append(const DevCache& c, const DevBatch& b, int d, const DevRope& r,
                                const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -557,9 +568,8 @@ hipError_t launch_cache_append(const DevCache& c, const DevBatch& b, int d, cons
   a.v_stride = v_stride;
   a.q_stride = q_stride;
   a.Hq = Hq;
-  a.page_wgs = int64_t(item_base(b.n_tokens, b.B, c.page, 2)) * c.H * (1 + (c.page + kPiece - 1) / kPiece);
-  const int64_t units = q ? int64_t(b.n_tokens) * ((Hq + kHeads - 1) / kHeads) * (d / 16) : 0;
-  const int64_t wgs = a.page_wgs + (units + kThreads - 1) / kThreads;
+  a.page_wgs = page_workgroups(c, b);
+  const int64_t wgs = a.page_wgs + query_workgroups(b, d, Hq);
   const auto kernel = d == 128 ? (c.fp4 ? cache_append_kernel<128, true> : cache_append_kernel<128, false>)
                                : (c.fp4 ? cache_append_kernel<64, true> : cache_append_kernel<64, false>);
   return launch_parts(kernel, a, wgs, 1, kThreads, 0, s);

@@ -22,9 +22,9 @@
 //
 // Scores are bound by the means' bytes (d bf16 a page and head), in short launches by the
 // latency of one chain: offsets, table, means, product. The search makes about 20 passes over
-// a row's scores, which a wave holds in registers, each waiting for the last. Measured: 16 sequences of up to 1024 pages,
-// 8 heads of 128, one query each: scores 12 us (18 MB), search 12; 3890 queries, 2 heads of
-// 64, 513 pages: 21 and 31.
+// a row's scores, which a wave holds in registers, each waiting for the last. Measured: 16
+// sequences of up to 1024 pages, 8 heads of 128, one query each: scores 13 us (18 MB), search
+// 11; 3890 queries, 2 heads of 64, 513 pages: 20 and 31.
 #include "cache.h"
 
 namespace spade {
@@ -616,6 +616,11 @@ hipError_t run(SelectArgs& a, const Plan& p, hipStream_t s) {
 static_assert(kCacheMaxPages <= 1024 * kMaxVals, "sixteen waves hold the longest row");
 
 }  // namespace
+
+bool cache_select_fits(const DevCache& c, const DevBatch& b) {
+  const Plan p = plan(c, b);
+  return int64_t(item_base(p.tokens, b.B, kTileQ, 1)) * c.H * p.chunks <= 0x7fffffff;
+}
 
 size_t cache_select_workspace_bytes(const DevCache& c, const DevBatch& b, int, int, int) {
   const Plan p = plan(c, b);

@@ -37,3 +37,9 @@ def test_attention():
     c, b = _structs(1, 1 << 22, 1 << 28, H=4096)
     assert _refused(S.lib().spade_cache_attn(ctypes.byref(c), ctypes.byref(b), FAKE, 4096, None, None, 0, 1,
                                              0.1, 0x2000, None, FAKE, 1 << 50, None), b"batch too large")
+
+
+def test_selection():
+    c, b = _structs(1 << 20, 8, 1, H=4096)
+    assert _refused(S.lib().spade_cache_select(ctypes.byref(c), ctypes.byref(b), FAKE, 4096, 4, 0, 1, 1, FAKE,
+                                               FAKE, FAKE, 1 << 50, None), b"batch too large")
