@@ -44,3 +44,25 @@ def test_large_values(L, n, H, fp4):
                                   C.stored(x.v[0][:, h:h + 1], fp4), [seen[i] for i in pick], None, 32, 0.65)
         assert bool(((o.cpu()[pick][:, h:h + 1].double() - ro).abs() <= ot).all()), h
         assert bool(((lse.cpu()[pick][:, h:h + 1].double() - rl).abs() <= lt).all()), h
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("L,n,H", [(500, 1, 2), (3000, 1, 1), (600, 256, 64)])
+def test_small_values(L, n, H, fp4):
+    """Values down to 2^-110: every one between that and 2^-104."""
+    print("small values", L, n, H, fp4, flush=True)
+    x = _rising(L, n, H, 32, fp4, 1.0)
+    gen = torch.Generator().manual_seed(6)
+    size = 2.0 ** (-110 + 6 * torch.rand(L, H, 64, generator=gen, dtype=torch.float64))
+    x.v[0] = (size * (1 - 2 * torch.randint(0, 2, size.shape, generator=gen))).to(torch.bfloat16)
+    x.hold([L])
+    x.to_device()
+    o = torch.empty(n, H, 64, dtype=torch.bfloat16, device=DEV)
+    S.spade_cache_attn(x.c, x.b, x.q.to(DEV), 0.65, o, workspace=x.workspace())
+    torch.cuda.synchronize()
+    pick = sorted({0, n // 3, n - 1})
+    seen = C.seen_by(L, n, True)
+    for h in {0, H - 1}:
+        ro, _, ot, _ = C.attend(x.q[pick][:, h:h + 1], C.stored(x.k[0][:, h:h + 1], fp4),
+                                C.stored(x.v[0][:, h:h + 1], fp4), [seen[i] for i in pick], None, 32, 0.65)
+        assert bool(((o.cpu()[pick][:, h:h + 1].double() - ro).abs() <= ot).all()), h
